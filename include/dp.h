@@ -356,6 +356,95 @@ size_t dp_kmeans_fit_workspace_bytes(const dp_prefill *in);
 dp_status dp_kmeans_fit(const dp_prefill *in, void *centroids, int32_t n_iters, uint32_t init, int32_t *assignment,
                         float *best_score, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- paged cache: tokens decoded after the prompt was clustered, and layers that stay dense ---- */
+
+/* A pool of pages of page_size tokens each and, per sequence, the list of the pages that hold its tokens.  Token i of
+ * sequence s lies in slot i % page_size of page page_table[s * table_stride + i / page_size]; its row of KV head h starts
+ * at element page * page_stride + h * head_stride + slot * slot_stride of k_pages and v_pages (so a pool may keep the
+ * heads or the tokens of a page outermost, or K and V of a page side by side).
+ *   seq_lens    tokens of each sequence; larger values than max_seq_len are clamped to it, negative ones to 0
+ *   page_table  an entry outside [0, n_pages) is a page that is not there: nothing is written to it, and its tokens
+ *               are left out of attention.  Entries behind the last token of a sequence are not read.
+ * Two sequences may share pages (dp_shared_prefix_decode). */
+typedef struct {
+  int32_t n_seqs, n_kv_heads, n_q_heads, head_dim; /* n_q_heads % n_kv_heads == 0; head_dim == 128        */
+  int32_t n_pages, page_size;                      /* page_size a power of two                            */
+  int64_t page_stride, head_stride, slot_stride;   /* elements; multiples of 8, not negative              */
+  void *k_pages, *v_pages;                         /* bf16, 16-byte aligned                               */
+  const int32_t *page_table;                       /* [n_seqs, table_stride]                              */
+  int32_t table_stride;
+  int32_t max_seq_len;                             /* host-known; <= table_stride * page_size             */
+  const int32_t *seq_lens;                         /* [n_seqs]                                            */
+  float sm_scale;                                  /* logit scale; 0 => 1/sqrt(head_dim)                  */
+} dp_paged_cache;
+
+/* New tokens for a paged cache.  The tokens of sequence s are [tok_ptr[s], tok_ptr[s+1]) (tok_ptr NULL: one token per
+ * sequence, n_tokens == n_seqs); they are the LAST tokens of their sequence: cache->seq_lens counts them already, token
+ * tok_ptr[s+1] - 1 goes to place seq_lens[s] - 1.  A token that no sequence holds (in front of tok_ptr[0], behind
+ * tok_ptr[n_seqs]) is skipped: neither the cache nor its row of q_out is written.  A token whose place lies outside
+ * [0, max_seq_len) or on a page that is not there is rotated (q_out) and not stored.
+ *   q, k, v   [n_tokens, heads, head_dim] of dtype, a token every q_stride (k_stride, v_stride) elements, its heads next
+ *             to each other: slices of one projection's output.  16-byte aligned, strides multiples of 16 bytes.
+ *   q_out     bf16 [n_tokens, n_q_heads, head_dim]; may be q itself where that is bf16 and contiguous
+ * Rotation of k and q to the token's position p (positions[token], or its place in the sequence): the first rope_dims
+ * dimensions form pairs i, dimensions (i, i + rope_dims/2), with DP_ROPE_ADJACENT_PAIRS (2i, 2i + 1), and
+ *   (a, b) -> (a cos t - b sin t, a sin t + b cos t),   t = p * rope_freqs[i]
+ * with t taken and reduced to a turn in 64 bits (an angle of 100000 radians in fp32 is off by 0.004), the products in
+ * fp32, one rounding to bf16; the other dimensions, and v, are copied (rounded from fp32). */
+#define DP_ROPE_ADJACENT_PAIRS 1u
+typedef struct {
+  int32_t n_tokens;
+  int32_t dtype;                        /* of q, k, v: DP_BF16 or DP_F32                                    */
+  const void *q, *k, *v;                /* q nullable: keys and values only                                 */
+  void *q_out;                          /* not read or written where q is NULL                              */
+  int64_t q_stride, k_stride, v_stride; /* elements between tokens                                          */
+  const int32_t *tok_ptr;               /* [n_seqs+1] or NULL                                               */
+  const int32_t *positions;             /* [n_tokens] or NULL                                               */
+  const float *rope_freqs;              /* [rope_dims / 2], radians per position; NULL where rope_dims == 0 */
+  int32_t rope_dims;                    /* 0, or a multiple of 16 up to head_dim                            */
+  uint32_t flags;                       /* DP_ROPE_*                                                        */
+} dp_kv_append;
+
+/* Stores the new tokens' keys (rotated) and values in the pages of the cache and the rotated queries in q_out.  Nothing
+ * else of the pool is written.  Two tokens with the same place, or two sequences that append to one page's slot, leave
+ * one of the two there.  Bitwise reproducible.  n_tokens == 0 does nothing. */
+dp_status dp_append_kv(const dp_paged_cache *cache, const dp_kv_append *tokens, void *stream);
+
+/* Dense attention (Sec. 2.1, Eq. 1) of one query token per sequence over rows [first_rows[s], seq_lens[s]) of its pages
+ * (first_rows NULL: from 0; negative values count as 0), for all query heads of a GQA group at once (any group size).
+ * What a step over the clustered prompt left (out and lse of dp_decode_attention in fp32) is joined where prior_out and
+ * prior_lse are given (both or neither): the result is attention over both parts,
+ *   out = (e^prior_lse prior_out + Z o) / (e^prior_lse + Z),  lse = ln(e^prior_lse + Z),
+ * Z and o the normaliser and the output of the pages' rows.  prior_out may be out, prior_lse may be lse.
+ *   q          bf16 [n_seqs, n_q_heads, head_dim], 16-byte aligned
+ *   out, lse   as dp_sparse_decode; no row and no prior (prior_lse = -inf): out = 0, lse = -inf
+ * Rows behind a sequence's last token (the rest of its last page) may hold anything, NaN included.
+ * workspace: dp_paged_workspace_bytes (0 for an invalid cache), 256-byte aligned. */
+size_t dp_paged_workspace_bytes(const dp_paged_cache *cache);
+dp_status dp_paged_decode(const dp_paged_cache *cache, const void *q, const int32_t *first_rows, const float *prior_out,
+                          const float *prior_lse, void *out, dp_dtype out_dtype, float *lse, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/* Groups of sequences that begin with the same tokens: the sequences [group_ptr[g], group_ptr[g+1]) share their first
+ * shared_lens[g] rows.  seq_lens counts them, and the page tables hold them: whole pages are usually the same in all
+ * tables of a group, a page in which the shared rows end is every sequence's own copy.
+ * A sequence shorter than its group's shared rows (an idle slot of the batch), one that no group holds and one beyond
+ * max_group_seqs in its group share nothing: they are attended through their own table alone, as all others are behind
+ * the shared rows. */
+typedef struct {
+  int32_t n_groups;
+  int32_t max_group_seqs, max_shared_len; /* host-known bounds; max_shared_len <= the cache's max_seq_len */
+  const int32_t *group_ptr;               /* [n_groups+1], ascending                                      */
+  const int32_t *shared_lens;             /* [n_groups]; clamped to [0, max_shared_len]                   */
+} dp_shared_prefix;
+
+/* dp_paged_decode (all rows, no prior) with the shared rows of a group read once for all its sequences, through the
+ * table of its first sequence that is long enough to hold them. */
+size_t dp_shared_prefix_workspace_bytes(const dp_paged_cache *cache, const dp_shared_prefix *prefix);
+dp_status dp_shared_prefix_decode(const dp_paged_cache *cache, const dp_shared_prefix *prefix, const void *q, void *out,
+                                  dp_dtype out_dtype, float *lse, void *workspace, size_t workspace_bytes,
+                                  void *stream);
+
 /* Where dp_decode_attention keeps its intermediate results inside the
  * workspace (byte offsets; host-only, for inspection by tests and tools):
  * logits as in dp_score_centroids, sel_ids as in dp_topp_select. */

@@ -30,6 +30,8 @@ EXPORTS = ["dp_workspace_bytes", "dp_logits_count", "dp_get_workspace_layout", "
            "dp_decode_attention_timed", "dp_budget_decode_attention", "dp_dense_decode", "dp_build_workspace_bytes", "dp_build_cluster_cache", "dp_kmeans_workspace_bytes",
            "dp_kmeans_assign", "dp_kmeans_fit_workspace_bytes", "dp_kmeans_fit",
            "dp_decode_attention_static", "dp_stream_read_probe", "dp_decode_attention_launches",
+           "dp_append_kv", "dp_paged_workspace_bytes", "dp_paged_decode", "dp_shared_prefix_workspace_bytes",
+           "dp_shared_prefix_decode",
            "dp_status_string"]
 
 
@@ -61,6 +63,28 @@ class _Layout(C.Structure):
     _fields_ = [("logits", C.c_size_t), ("sel_ids", C.c_size_t), ("row_start", C.c_size_t),
                 ("chunk_entry", C.c_size_t), ("counts", C.c_size_t), ("partials", C.c_size_t),
                 ("total", C.c_size_t), ("splits", C.c_int32), ("chunk_rows", C.c_int32), ("summaries", C.c_size_t)]
+
+
+class _PagedCache(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_kv_heads", C.c_int32), ("n_q_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("slot_stride", C.c_int64),
+                ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_table", C.c_void_p),
+                ("table_stride", C.c_int32), ("max_seq_len", C.c_int32), ("seq_lens", C.c_void_p),
+                ("sm_scale", C.c_float)]
+
+
+class _KvAppend(C.Structure):
+    _fields_ = [("n_tokens", C.c_int32), ("dtype", C.c_int32),
+                ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_out", C.c_void_p),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("tok_ptr", C.c_void_p), ("positions", C.c_void_p), ("rope_freqs", C.c_void_p),
+                ("rope_dims", C.c_int32), ("flags", C.c_uint32)]
+
+
+class _SharedPrefix(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("max_group_seqs", C.c_int32), ("max_shared_len", C.c_int32),
+                ("group_ptr", C.c_void_p), ("shared_lens", C.c_void_p)]
 
 
 _lib = None
@@ -128,6 +152,17 @@ def load_library():
     L.dp_decode_attention_launches.argtypes = [PP]
     L.dp_stream_read_probe.restype = I
     L.dp_stream_read_probe.argtypes = [V, C.c_size_t, V, V, V, V]
+    PC = C.POINTER(_PagedCache)
+    L.dp_append_kv.restype = I
+    L.dp_append_kv.argtypes = [PC, C.POINTER(_KvAppend), V]
+    L.dp_paged_workspace_bytes.restype = C.c_size_t
+    L.dp_paged_workspace_bytes.argtypes = [PC]
+    L.dp_paged_decode.restype = I
+    L.dp_paged_decode.argtypes = [PC, V, V, V, V, V, I, V, V, C.c_size_t, V]
+    L.dp_shared_prefix_workspace_bytes.restype = C.c_size_t
+    L.dp_shared_prefix_workspace_bytes.argtypes = [PC, C.POINTER(_SharedPrefix)]
+    L.dp_shared_prefix_decode.restype = I
+    L.dp_shared_prefix_decode.argtypes = [PC, C.POINTER(_SharedPrefix), V, V, I, V, V, C.c_size_t, V]
     L.dp_status_string.restype = C.c_char_p
     L.dp_status_string.argtypes = [I]
     _lib = L
@@ -497,3 +532,188 @@ def dp_kmeans_fit(prefill: Prefill, centroids: torch.Tensor, n_iters: int, init:
                                         _ptr(best_score), _ptr(workspace),
                                         workspace.numel() * workspace.element_size(), _stream(stream)),
            "dp_kmeans_fit")
+
+
+# ---- paged cache ----
+
+def _dense_rows(t: torch.Tensor, heads: int) -> bool:
+    """[n, heads, 128] with the heads of a token next to each other (any stride between tokens)."""
+    return t.dim() == 3 and t.shape[1:] == (heads, 128) and (t.numel() == 0 or t.stride()[1:] == (128, 1) or
+                                                             (heads == 1 and t.stride(2) == 1))
+
+
+def _on(device: torch.device, *tensors: Optional[torch.Tensor]) -> None:
+    for t in tensors:
+        assert t is None or t.device == device, f"tensor on {t.device}, the cache is on {device}"
+
+
+class PagedCache:
+    """Host-side dp_paged_cache over device tensors.
+
+    k_pages, v_pages  bf16 (or their raw int16 bits) [n_pages, n_kv_heads, page_size, 128], the same strides, a row's 128
+                      values adjacent: a pool with the tokens outermost in a page is passed as pages.transpose(1, 2)
+    page_table        int32 [n_seqs, pages per sequence]; seq_lens  int32 [n_seqs], both read by the kernels at every call
+    max_seq_len       upper bound of seq_lens, known to the host
+    """
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor,
+                 max_seq_len: int, n_q_heads: int, sm_scale: float = 0.0):
+        assert k_pages.dim() == 4 and k_pages.shape == v_pages.shape and k_pages.stride() == v_pages.stride()
+        assert k_pages.dtype == v_pages.dtype and k_pages.dtype in (torch.bfloat16, torch.int16)
+        assert k_pages.numel() == 0 or k_pages.stride(3) == 1
+        assert page_table.dtype == torch.int32 and page_table.dim() == 2
+        assert page_table.numel() == 0 or page_table.stride(1) == 1 or page_table.shape[1] == 1
+        assert seq_lens.dtype == torch.int32 and seq_lens.is_contiguous() and seq_lens.numel() == page_table.shape[0]
+        self.device = k_pages.device
+        _on(self.device, v_pages, page_table, seq_lens)
+        self.k_pages, self.v_pages, self.page_table, self.seq_lens = k_pages, v_pages, page_table, seq_lens
+        self.n_seqs, self.n_kv_heads, self.n_q_heads = int(page_table.shape[0]), int(k_pages.shape[1]), int(n_q_heads)
+        n_pages, _, page_size, dim = k_pages.shape
+        # (one line: its stride says nothing; lines that overlap would not be lines)
+        line = page_table.stride(0) if page_table.shape[0] > 1 else page_table.shape[1]
+        assert line >= page_table.shape[1] and int(max_seq_len) <= page_table.shape[1] * page_size
+        self.c = _PagedCache(self.n_seqs, self.n_kv_heads, self.n_q_heads, dim, n_pages, page_size, k_pages.stride(0),
+                             k_pages.stride(1), k_pages.stride(2), _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
+                             line, int(max_seq_len), _ptr(seq_lens), float(sm_scale))
+
+    @property
+    def ref(self):
+        return C.byref(self.c)
+
+
+class SharedPrefix:
+    """Host-side dp_shared_prefix: group_ptr int32 [n_groups + 1], shared_lens int32 [n_groups] on the device, and the
+    host-known bounds on a group's sequences and on its shared rows."""
+
+    def __init__(self, group_ptr: torch.Tensor, shared_lens: torch.Tensor, max_group_seqs: int, max_shared_len: int):
+        for t in (group_ptr, shared_lens):
+            assert t.dtype == torch.int32 and t.is_contiguous()
+        assert group_ptr.numel() == shared_lens.numel() + 1
+        self.tensors = (group_ptr, shared_lens)
+        self.c = _SharedPrefix(shared_lens.numel(), int(max_group_seqs), int(max_shared_len), _ptr(group_ptr),
+                               _ptr(shared_lens))
+
+    @property
+    def ref(self):
+        return C.byref(self.c)
+
+
+def _enqueue(name: str, fn, args, device: torch.device, stream) -> None:
+    """fn(*args, stream) on `device`, which need not be the current one; stream None: the one current there now."""
+    if torch.cuda.current_device() != device.index:
+        with torch.cuda.device(device):
+            return _enqueue(name, fn, args, device, stream)
+    _check(fn(*args, _stream(stream)), name)
+
+
+def _paged_entry(marshal):
+    """An entry point over a paged cache: marshal checks and converts the arguments, the call enqueues."""
+    name = marshal.__name__
+
+    def call(*args, stream=None, **kw) -> None:
+        c_args, device, _keep = marshal(*args, **kw)
+        assert device.type == "cuda", f"{name} needs a GPU (there is no CPU fallback)"
+        _enqueue(name, getattr(load_library(), name), c_args, device, stream)
+
+    call.__name__ = call.__qualname__ = name
+    call.__doc__ = marshal.__doc__
+    call.marshal = marshal
+    return call
+
+
+class BoundCall:
+    """An entry point over a paged cache with its arguments checked and converted once: calling the object enqueues the
+    call (a serving loop makes the same call every step; converting the same pointers again costs the host more than a
+    small call takes).  The tensors are kept alive by the object and must not be resized; what the kernels read from them
+    (queries, page table, lengths) may change between calls.  ``stream`` (default: the stream current at each call)."""
+
+    def __init__(self, entry, *args, stream=None, **kw):
+        c_args, self._device, self._keep = entry.marshal(*args, **kw)
+        assert self._device.type == "cuda", f"{entry.__name__} needs a GPU (there is no CPU fallback)"
+        self._name, self._fn, self._stream = entry.__name__, getattr(load_library(), entry.__name__), stream
+        # ctypes converts at every call what is not one of its own objects yet
+        self._args = tuple(t(a) if t in (C.c_void_p, C.c_int, C.c_size_t) else a
+                           for t, a in zip(self._fn.argtypes, c_args))
+
+    def __call__(self) -> None:
+        _enqueue(self._name, self._fn, self._args, self._device, self._stream)
+
+
+@_paged_entry
+def dp_append_kv(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, rope_freqs: Optional[torch.Tensor] = None,
+                 q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                 tok_ptr: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                 adjacent_pairs: bool = False):
+    """New tokens into the pages: k, v (and q, rotated into q_out) [n_tokens, heads, 128], bf16 or fp32, any stride between
+    tokens.  tok_ptr int32 [n_seqs + 1] (None: one token per sequence); cache.seq_lens counts the new tokens already.
+    rope_freqs fp32 [rope_dims / 2], None or empty: no rotation.  positions int32 [n_tokens]: where a token's position is
+    not its place in the sequence."""
+    n = k.shape[0]
+    dt = {torch.float32: DP_F32, torch.bfloat16: DP_BF16}[k.dtype]
+    assert k.dtype == v.dtype and v.shape[0] == n
+    assert _dense_rows(k, cache.n_kv_heads) and _dense_rows(v, cache.n_kv_heads)
+    if q is not None:
+        assert q.dtype == k.dtype and q.shape[0] == n and _dense_rows(q, cache.n_q_heads)
+        assert q_out is not None and q_out.dtype == torch.bfloat16 and q_out.is_contiguous() and q_out.numel() == q.numel()
+    if tok_ptr is None:
+        assert n == cache.n_seqs, "one token per sequence where there is no tok_ptr"
+    else:
+        assert tok_ptr.dtype == torch.int32 and tok_ptr.is_contiguous() and tok_ptr.numel() == cache.n_seqs + 1
+    assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() >= n)
+    half = 0 if rope_freqs is None else rope_freqs.numel()
+    assert half == 0 or (rope_freqs.dtype == torch.float32 and rope_freqs.is_contiguous())
+    _on(cache.device, k, v, q, q_out, tok_ptr, positions, rope_freqs)
+    stride = lambda t: 0 if t is None or n < 2 else t.stride(0)  # noqa: E731
+    new = _KvAppend(n, dt, None if q is None else _ptr(q), _ptr(k), _ptr(v), None if q is None else _ptr(q_out), stride(q),
+                    stride(k), stride(v), _ptr(tok_ptr), _ptr(positions), None if half == 0 else _ptr(rope_freqs),
+                    2 * half, 1 if adjacent_pairs else 0)
+    return (cache.ref, C.byref(new)), cache.device, (cache, new, k, v, rope_freqs, q, q_out, tok_ptr, positions)
+
+
+def dp_paged_workspace_bytes(cache: PagedCache) -> int:
+    return int(load_library().dp_paged_workspace_bytes(cache.ref))
+
+
+def dp_shared_prefix_workspace_bytes(cache: PagedCache, prefix: SharedPrefix) -> int:
+    return int(load_library().dp_shared_prefix_workspace_bytes(cache.ref, prefix.ref))
+
+
+def _attention_buffers(cache: PagedCache, q, out, lse, workspace) -> int:
+    n = cache.n_seqs * cache.n_q_heads
+    assert q.dtype in (torch.bfloat16, torch.int16) and q.is_contiguous() and q.numel() == n * 128
+    assert out.is_contiguous() and out.numel() == n * 128
+    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == n)
+    assert workspace.is_contiguous()
+    _on(cache.device, q, out, lse, workspace)
+    return {torch.float32: DP_F32, torch.bfloat16: DP_BF16}[out.dtype]
+
+
+@_paged_entry
+def dp_paged_decode(cache: PagedCache, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor],
+                    workspace: torch.Tensor, first_rows: Optional[torch.Tensor] = None,
+                    prior_out: Optional[torch.Tensor] = None, prior_lse: Optional[torch.Tensor] = None):
+    """Attention of one query token per sequence over rows [first_rows[s], seq_lens[s]) of its pages, joined with
+    (prior_out, prior_lse), fp32, where they are given."""
+    dt = _attention_buffers(cache, q, out, lse, workspace)
+    assert first_rows is None or (first_rows.dtype == torch.int32 and first_rows.is_contiguous() and
+                                  first_rows.numel() == cache.n_seqs)
+    assert (prior_out is None) == (prior_lse is None)
+    if prior_out is not None:
+        n = cache.n_seqs * cache.n_q_heads
+        assert prior_out.dtype == torch.float32 and prior_out.is_contiguous() and prior_out.numel() == n * 128
+        assert prior_lse.dtype == torch.float32 and prior_lse.is_contiguous() and prior_lse.numel() == n
+    _on(cache.device, first_rows, prior_out, prior_lse)
+    return ((cache.ref, _ptr(q), _ptr(first_rows), _ptr(prior_out), _ptr(prior_lse), _ptr(out), dt, _ptr(lse),
+             _ptr(workspace), workspace.numel() * workspace.element_size()), cache.device,
+            (cache, q, out, lse, workspace, first_rows, prior_out, prior_lse))
+
+
+@_paged_entry
+def dp_shared_prefix_decode(cache: PagedCache, prefix: SharedPrefix, q: torch.Tensor, out: torch.Tensor,
+                            lse: Optional[torch.Tensor], workspace: torch.Tensor):
+    """dp_paged_decode over all rows of a batch whose groups of sequences share their first rows: those are read once per
+    group."""
+    dt = _attention_buffers(cache, q, out, lse, workspace)
+    _on(cache.device, *prefix.tensors)
+    return ((cache.ref, prefix.ref, _ptr(q), _ptr(out), dt, _ptr(lse), _ptr(workspace),
+             workspace.numel() * workspace.element_size()), cache.device, (cache, prefix, q, out, lse, workspace))

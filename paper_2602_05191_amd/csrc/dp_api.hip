@@ -266,6 +266,57 @@ dp_status static_scratch(void **ptr) {
   return DP_OK;
 }
 
+// ---- paged cache ----
+constexpr int64_t kMaxPagedHeads = 1 << 22;  // sequences x query heads of a call (grid sizes stay below 2^32 threads)
+
+bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+dp_status paged_ok(const dp_paged_cache *c) {
+  if (!c || c->n_seqs <= 0 || c->n_kv_heads <= 0 || c->n_q_heads <= 0 || c->n_q_heads % c->n_kv_heads ||
+      c->n_pages < 0 || c->page_size <= 0 || c->page_stride < 0 || c->head_stride < 0 || c->slot_stride < 0 ||
+      c->page_stride % 8 || c->head_stride % 8 || c->slot_stride % 8 || c->table_stride < 0 || c->max_seq_len < 0 ||
+      (int64_t)c->table_stride * c->page_size < c->max_seq_len || c->sm_scale < 0.0f || c->sm_scale != c->sm_scale ||
+      !c->seq_lens || (c->max_seq_len > 0 && !c->page_table) ||
+      (c->n_pages > 0 && (!c->k_pages || !c->v_pages || !aligned16(c->k_pages) || !aligned16(c->v_pages))))
+    return DP_ERR_INVALID_ARG;
+  if (c->head_dim != dp::kHeadDim || (c->page_size & (c->page_size - 1)) ||
+      (int64_t)c->n_seqs * c->n_q_heads > kMaxPagedHeads)
+    return DP_ERR_UNSUPPORTED;
+  // the places of a pool fit 64 bits, those of a head's rows inside a page 31
+  constexpr int64_t kMost = (int64_t)1 << 58;
+  constexpr int64_t kMostInPage = (int64_t)1 << 30;
+  if (c->slot_stride > kMostInPage || (c->page_size - 1) * c->slot_stride + dp::kHeadDim > kMostInPage ||
+      c->head_stride > kMost / c->n_kv_heads || c->page_stride > kMost / (c->n_pages + 1))
+    return DP_ERR_UNSUPPORTED;
+  return DP_OK;
+}
+
+dp::PagedView view_of(const dp_paged_cache *c) {
+  dp::PagedView v;
+  v.n_seqs = c->n_seqs;
+  v.n_kv_heads = c->n_kv_heads;
+  v.n_q_heads = c->n_q_heads;
+  v.group = c->n_q_heads / c->n_kv_heads;
+  v.n_pages = c->n_pages;
+  v.page_shift = __builtin_ctz((unsigned)c->page_size);
+  v.page_stride = c->page_stride * 2;
+  v.head_stride = c->head_stride * 2;
+  v.slot_stride = (uint32_t)(c->slot_stride * 2);
+  v.k_pages = static_cast<char *>(c->k_pages);
+  v.v_pages = static_cast<char *>(c->v_pages);
+  v.table = c->page_table;
+  v.seq_lens = c->seq_lens;
+  v.table_stride = c->table_stride;
+  v.max_seq_len = c->n_pages > 0 ? c->max_seq_len : 0;  // (a pool without pages holds no token)
+  v.sm_scale = c->sm_scale != 0.0f ? c->sm_scale : 1.0f / sqrtf((float)c->head_dim);
+  return v;
+}
+
+bool prefix_ok(const dp_paged_cache *c, const dp_shared_prefix *p) {
+  return p && p->n_groups > 0 && p->max_group_seqs > 0 && p->max_shared_len >= 0 &&
+         p->max_shared_len <= c->max_seq_len && p->group_ptr && p->shared_lens;
+}
+
 }  // namespace
 
 extern "C" {
@@ -629,6 +680,78 @@ dp_status dp_kmeans_fit(const dp_prefill *in, void *centroids, int32_t n_iters, 
     if (dp::launch_build(b, workspace, s) != hipSuccess) return DP_ERR_HIP;
   }
   return DP_OK;
+}
+
+dp_status dp_append_kv(const dp_paged_cache *cache, const dp_kv_append *tokens, void *stream) {
+  const dp_status st = paged_ok(cache);
+  if (st != DP_OK) return st;
+  if (!tokens || tokens->n_tokens < 0 || (tokens->flags & ~DP_ROPE_ADJACENT_PAIRS)) return DP_ERR_INVALID_ARG;
+  if ((tokens->dtype != DP_BF16 && tokens->dtype != DP_F32) || tokens->rope_dims < 0 ||
+      tokens->rope_dims > dp::kHeadDim || tokens->rope_dims % 16)
+    return DP_ERR_UNSUPPORTED;
+  if (!tokens->tok_ptr && tokens->n_tokens != cache->n_seqs && tokens->n_tokens != 0) return DP_ERR_INVALID_ARG;
+  if (tokens->n_tokens == 0) return DP_OK;
+  if (!tokens->k || !tokens->v || (tokens->q && !tokens->q_out) || (tokens->rope_dims > 0 && !tokens->rope_freqs))
+    return DP_ERR_INVALID_ARG;
+  const int size = tokens->dtype == DP_F32 ? 4 : 2;
+  const int64_t strides[3] = {tokens->k_stride, tokens->v_stride, tokens->q ? tokens->q_stride : 0};
+  for (int64_t stride : strides)
+    if (stride < 0 || stride * size % 16 || stride > ((int64_t)1 << 58) / tokens->n_tokens) return DP_ERR_INVALID_ARG;
+  if (!aligned16(tokens->k) || !aligned16(tokens->v) || (tokens->q && (!aligned16(tokens->q) || !aligned16(tokens->q_out))))
+    return DP_ERR_INVALID_ARG;
+  dp::AppendTokens t;
+  t.n_tokens = tokens->n_tokens;
+  t.is_f32 = tokens->dtype == DP_F32;
+  t.q = tokens->q;
+  t.k = tokens->k;
+  t.v = tokens->v;
+  t.q_out = tokens->q ? tokens->q_out : nullptr;
+  t.q_stride = tokens->q_stride * size;
+  t.k_stride = tokens->k_stride * size;
+  t.v_stride = tokens->v_stride * size;
+  t.tok_ptr = tokens->tok_ptr;
+  t.positions = tokens->positions;
+  t.freqs = tokens->rope_freqs;
+  t.rope_dims = tokens->rope_dims;
+  t.adjacent = (tokens->flags & DP_ROPE_ADJACENT_PAIRS) != 0;
+  return dp::launch_append(view_of(cache), t, static_cast<hipStream_t>(stream)) == hipSuccess ? DP_OK : DP_ERR_HIP;
+}
+
+size_t dp_paged_workspace_bytes(const dp_paged_cache *cache) { return paged_ok(cache) == DP_OK ? 256 : 0; }
+
+dp_status dp_paged_decode(const dp_paged_cache *cache, const void *q, const int32_t *first_rows, const float *prior_out,
+                          const float *prior_lse, void *out, dp_dtype out_dtype, float *lse, void *workspace,
+                          size_t workspace_bytes, void *stream) {
+  const dp_status st = paged_ok(cache);
+  if (st != DP_OK) return st;
+  if (out_dtype != DP_BF16 && out_dtype != DP_F32) return DP_ERR_UNSUPPORTED;
+  if (!q || !aligned16(q) || !out || !workspace || !prior_out != !prior_lse) return DP_ERR_INVALID_ARG;
+  if (workspace_bytes < dp_paged_workspace_bytes(cache)) return DP_ERR_WORKSPACE_TOO_SMALL;
+  if (reinterpret_cast<uintptr_t>(workspace) % 256) return DP_ERR_INVALID_ARG;
+  const dp::PagedAttention a{q, first_rows, prior_out, prior_lse};
+  const dp::AttnOut attn{out, lse, out_dtype == DP_BF16};
+  return dp::launch_paged_decode(view_of(cache), a, attn, static_cast<hipStream_t>(stream)) == hipSuccess ? DP_OK
+                                                                                                         : DP_ERR_HIP;
+}
+
+size_t dp_shared_prefix_workspace_bytes(const dp_paged_cache *cache, const dp_shared_prefix *prefix) {
+  return paged_ok(cache) == DP_OK && prefix_ok(cache, prefix) ? 256 : 0;
+}
+
+dp_status dp_shared_prefix_decode(const dp_paged_cache *cache, const dp_shared_prefix *prefix, const void *q, void *out,
+                                  dp_dtype out_dtype, float *lse, void *workspace, size_t workspace_bytes,
+                                  void *stream) {
+  const dp_status st = paged_ok(cache);
+  if (st != DP_OK) return st;
+  if (!prefix_ok(cache, prefix)) return DP_ERR_INVALID_ARG;
+  if (out_dtype != DP_BF16 && out_dtype != DP_F32) return DP_ERR_UNSUPPORTED;
+  if (!q || !aligned16(q) || !out || !workspace) return DP_ERR_INVALID_ARG;
+  if (workspace_bytes < dp_shared_prefix_workspace_bytes(cache, prefix)) return DP_ERR_WORKSPACE_TOO_SMALL;
+  if (reinterpret_cast<uintptr_t>(workspace) % 256) return DP_ERR_INVALID_ARG;
+  const dp::PagedAttention a{q, nullptr, nullptr, nullptr};
+  const dp::AttnOut attn{out, lse, out_dtype == DP_BF16};
+  return dp::launch_paged_decode(view_of(cache), a, attn, static_cast<hipStream_t>(stream)) == hipSuccess ? DP_OK
+                                                                                                         : DP_ERR_HIP;
 }
 
 const char *dp_status_string(dp_status status) {

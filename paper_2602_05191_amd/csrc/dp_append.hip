@@ -1,0 +1,133 @@
+// Appending to a paged cache: keys rotated to their positions, values as they are, into the pages; queries rotated.
+//
+// Rotation of a pair (a, b) at position p with frequency f: (a cos t - b sin t, a sin t + b cos t), t = p f.  t is taken
+// in turns in 64 bits (p f / 2 pi, the nearest whole number of turns off), so the angle handed to the fp32 sine and cosine
+// is exact to 2^-25 of a turn whatever the position; products in fp32, one rounding to bf16.
+//
+// A wave owns one token (or one of `parts` shares of its rows): its 64 lanes find the token's sequence, page and slot
+// and take the sines and cosines of the up to 64 pairs, one each, which all heads of the token then share through LDS.
+// A row (one head) is 16 lanes x 8 dimensions, four rows per wave and load.
+#include "dp_kernels.hpp"
+#include "dp_paged_rows.hpp"
+
+namespace dp {
+namespace {
+
+constexpr int kAppendThreads = 256;
+constexpr int kAppendWaves = kAppendThreads / 64;
+
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// 8 dimensions of a row, widened
+template <bool kF32>
+struct Slice;
+template <>
+struct Slice<true> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const char *row, int lane16) {
+    const float4 *p = reinterpret_cast<const float4 *>(row) + 2 * lane16;
+    a = p[0];
+    b = p[1];
+  }
+  __device__ __forceinline__ void widen(float (&x)[8]) const {
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+};
+template <>
+struct Slice<false> {
+  uint4 a;
+  __device__ __forceinline__ void load(const char *row, int lane16) { a = reinterpret_cast<const uint4 *>(row)[lane16]; }
+  __device__ __forceinline__ void widen(float (&x)[8]) const { unpack8(a, x); }
+};
+
+__device__ __forceinline__ uint4 round8(const float (&x)[8]) {  // to nearest even, NaN stays NaN
+  const f32x8 v = {x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]};
+  return __builtin_bit_cast(uint4, __builtin_convertvector(v, bf16x8));
+}
+
+template <bool kF32>
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView c, AppendTokens t, int parts) {
+  __shared__ float2 s_turn[kAppendWaves][kHeadDim / 2];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
+  const int t16 = lane & 15, grp = lane >> 4;
+  const int64_t task = (int64_t)blockIdx.x * kAppendWaves + wave;
+  const int token = (int)min(task / parts, (int64_t)t.n_tokens - 1), part = (int)(task % parts);
+  bool live = task < (int64_t)t.n_tokens * parts;
+
+  const int found = t.tok_ptr ? wave_find(t.tok_ptr, c.n_seqs, token) : token;
+  live = live && found < c.n_seqs;
+  const int seq = min(found, c.n_seqs - 1);
+  const int64_t at = (int64_t)c.seq_lens[seq] - (t.tok_ptr ? (int64_t)t.tok_ptr[seq + 1] - token : 1);
+  bool stored = at >= 0 && at < c.max_seq_len;
+  int64_t page = 0;
+  if (stored) {
+    page = c.table[(int64_t)seq * c.table_stride + (at >> c.page_shift)];
+    stored = page >= 0 && page < c.n_pages;
+  }
+  const int64_t place = page * c.page_stride + (at & ((1 << c.page_shift) - 1)) * c.slot_stride;
+  const double position = t.positions ? (double)t.positions[token] : (double)at;
+
+  const int half = t.rope_dims / 2;
+  if (lane < half) {
+    const double turns = position * ((double)t.freqs[lane] * 0.15915494309189535);  // 1 / 2 pi
+    float2 cs;
+    sincospif(2.f * (float)(turns - rint(turns)), &cs.y, &cs.x);
+    s_turn[wave][lane] = cs;
+  }
+  __syncthreads();
+  if (!live) return;
+
+  // what the lane's 8 dimensions are multiplied with, and the partner dimension of each
+  const int lanes_half = half / 8;  // lanes that hold the first dimensions of the pairs (i, i + half)
+  const bool turns = t16 < 2 * lanes_half;
+  float cosine[8], sine[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int pair = t.adjacent ? 4 * t16 + e / 2 : 8 * (t16 < lanes_half ? t16 : t16 - lanes_half) + e;
+    const float2 cs = s_turn[wave][turns ? pair : 0];
+    const bool first = t.adjacent ? e % 2 == 0 : t16 < lanes_half;
+    cosine[e] = cs.x;
+    sine[e] = first ? -cs.y : cs.y;
+  }
+  const int partner = (lane & 48) + (!turns ? t16 : t16 < lanes_half ? t16 + lanes_half : t16 - lanes_half);
+
+  const int n_kv = c.n_kv_heads, rows = 2 * n_kv + (t.q ? c.n_q_heads : 0);
+  for (int r0 = 4 * part; r0 < rows; r0 += 4 * parts) {  // keys, values, queries
+    const int r = min(r0 + grp, rows - 1);
+    const bool is_v = r >= n_kv && r < 2 * n_kv, is_q = r >= 2 * n_kv;
+    const int head = is_q ? r - 2 * n_kv : is_v ? r - n_kv : r;
+    const char *src = static_cast<const char *>(is_q ? t.q : is_v ? t.v : t.k) +
+                      token * (is_q ? t.q_stride : is_v ? t.v_stride : t.k_stride) + head * (kHeadDim * (kF32 ? 4 : 2));
+    Slice<kF32> s;
+    s.load(src, t16);
+    float x[8], y[8];
+    s.widen(x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float other = t.adjacent ? x[e ^ 1] : __shfl(x[e], partner, 64);
+      const float turned = fmaf(x[e], cosine[e], other * sine[e]);
+      y[e] = turns && !is_v ? turned : x[e];
+    }
+    if (r0 + grp >= rows || (!is_q && !stored)) continue;
+    char *dst = is_q ? static_cast<char *>(t.q_out) + ((int64_t)token * c.n_q_heads + head) * kRowBytes
+                     : (is_v ? c.v_pages : c.k_pages) + place + head * c.head_stride;
+    reinterpret_cast<uint4 *>(dst)[t16] = round8(y);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_append(const PagedView &c, const AppendTokens &t, hipStream_t s) {
+  const int parts = 1;
+  const int64_t tasks = (int64_t)t.n_tokens * parts;
+  const dim3 grid((unsigned)((tasks + kAppendWaves - 1) / kAppendWaves)), block(kAppendThreads);
+  if (t.is_f32)
+    hipLaunchKernelGGL(append_kernel<true>, grid, block, 0, s, c, t, parts);
+  else
+    hipLaunchKernelGGL(append_kernel<false>, grid, block, 0, s, c, t, parts);
+  return hipGetLastError();
+}
+
+}  // namespace dp

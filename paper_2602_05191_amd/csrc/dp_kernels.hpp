@@ -129,6 +129,36 @@ hipError_t launch_group_decode(const CacheView &c, const int32_t *n_exact_u, con
 hipError_t launch_dense(const CacheView &c, const int32_t *seg_rows, float *partials, int max_splits,
                         const AttnOut &attn, hipStream_t s);
 
+// Paged cache (strides in bytes)
+struct PagedView {
+  int32_t n_seqs, n_kv_heads, n_q_heads, group;  // group = n_q_heads / n_kv_heads
+  int32_t n_pages, page_shift;                   // 1 << page_shift tokens per page
+  int64_t page_stride, head_stride;
+  uint32_t slot_stride;  // a page's rows of one head span less than 2^31 bytes
+  char *k_pages, *v_pages;
+  const int32_t *table, *seq_lens;
+  int32_t table_stride, max_seq_len;
+  float sm_scale;
+};
+
+struct AppendTokens {
+  int32_t n_tokens, is_f32;
+  const void *q, *k, *v;
+  void *q_out;
+  int64_t q_stride, k_stride, v_stride;  // bytes
+  const int32_t *tok_ptr, *positions;    // nullable
+  const float *freqs;
+  int32_t rope_dims, adjacent;
+};
+hipError_t launch_append(const PagedView &c, const AppendTokens &t, hipStream_t s);
+
+struct PagedAttention {
+  const void *q;
+  const int32_t *first_rows;              // nullable
+  const float *prior_out, *prior_lse;     // nullable
+};
+hipError_t launch_paged_decode(const PagedView &c, const PagedAttention &a, const AttnOut &attn, hipStream_t s);
+
 // Prefill side: token-order K / V + cluster ids -> cluster-contiguous cache and cluster metadata.
 struct BuildProblem {
   int32_t n_seg;
