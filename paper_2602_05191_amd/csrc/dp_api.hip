@@ -268,6 +268,7 @@ dp_status static_scratch(void **ptr) {
 
 // ---- paged cache ----
 constexpr int64_t kMaxPagedHeads = 1 << 22;  // sequences x query heads of a call (grid sizes stay below 2^32 threads)
+constexpr int32_t kMaxPagedLen = 1 << 30;    // rows of a sequence (a row number plus a round of tiles stays below 2^31)
 
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
@@ -280,7 +281,8 @@ dp_status paged_ok(const dp_paged_cache *c) {
       (c->n_pages > 0 && (!c->k_pages || !c->v_pages || !aligned16(c->k_pages) || !aligned16(c->v_pages))))
     return DP_ERR_INVALID_ARG;
   if (c->head_dim != dp::kHeadDim || (c->page_size & (c->page_size - 1)) ||
-      (int64_t)c->n_seqs * c->n_q_heads > kMaxPagedHeads)
+      (int64_t)c->n_seqs * c->n_q_heads > kMaxPagedHeads || c->max_seq_len > kMaxPagedLen ||
+      (int64_t)c->n_seqs * c->n_kv_heads * (c->max_seq_len / dp::kChunkRows + 1) >= (int64_t)1 << 30)
     return DP_ERR_UNSUPPORTED;
   // the places of a pool fit 64 bits, those of a head's rows inside a page 31
   constexpr int64_t kMost = (int64_t)1 << 58;
@@ -315,6 +317,19 @@ dp::PagedView view_of(const dp_paged_cache *c) {
 bool prefix_ok(const dp_paged_cache *c, const dp_shared_prefix *p) {
   return p && p->n_groups > 0 && p->max_group_seqs > 0 && p->max_shared_len >= 0 &&
          p->max_shared_len <= c->max_seq_len && p->group_ptr && p->shared_lens;
+}
+
+dp::SharedView view_of(const dp_shared_prefix *p) {
+  return dp::SharedView{p->n_groups, p->max_group_seqs, p->max_shared_len, p->group_ptr, p->shared_lens};
+}
+
+dp_status paged_attention(const dp_paged_cache *cache, const dp::PagedAttention &a, void *out, dp_dtype out_dtype,
+                          float *lse, void *workspace, void *stream) {
+  const dp::AttnOut attn{out, lse, out_dtype == DP_BF16};
+  return dp::launch_paged_decode(view_of(cache), a, static_cast<float *>(workspace), attn,
+                                 static_cast<hipStream_t>(stream)) == hipSuccess
+             ? DP_OK
+             : DP_ERR_HIP;
 }
 
 }  // namespace
@@ -717,7 +732,10 @@ dp_status dp_append_kv(const dp_paged_cache *cache, const dp_kv_append *tokens, 
   return dp::launch_append(view_of(cache), t, static_cast<hipStream_t>(stream)) == hipSuccess ? DP_OK : DP_ERR_HIP;
 }
 
-size_t dp_paged_workspace_bytes(const dp_paged_cache *cache) { return paged_ok(cache) == DP_OK ? 256 : 0; }
+size_t dp_paged_workspace_bytes(const dp_paged_cache *cache) {
+  if (paged_ok(cache) != DP_OK) return 0;
+  return align_up(sizeof(float) * dp::paged_partials(view_of(cache), dp::SharedView{}), 256);
+}
 
 dp_status dp_paged_decode(const dp_paged_cache *cache, const void *q, const int32_t *first_rows, const float *prior_out,
                           const float *prior_lse, void *out, dp_dtype out_dtype, float *lse, void *workspace,
@@ -728,14 +746,13 @@ dp_status dp_paged_decode(const dp_paged_cache *cache, const void *q, const int3
   if (!q || !aligned16(q) || !out || !workspace || !prior_out != !prior_lse) return DP_ERR_INVALID_ARG;
   if (workspace_bytes < dp_paged_workspace_bytes(cache)) return DP_ERR_WORKSPACE_TOO_SMALL;
   if (reinterpret_cast<uintptr_t>(workspace) % 256) return DP_ERR_INVALID_ARG;
-  const dp::PagedAttention a{q, first_rows, prior_out, prior_lse};
-  const dp::AttnOut attn{out, lse, out_dtype == DP_BF16};
-  return dp::launch_paged_decode(view_of(cache), a, attn, static_cast<hipStream_t>(stream)) == hipSuccess ? DP_OK
-                                                                                                         : DP_ERR_HIP;
+  return paged_attention(cache, dp::PagedAttention{q, first_rows, prior_out, prior_lse, dp::SharedView{}}, out,
+                         out_dtype, lse, workspace, stream);
 }
 
 size_t dp_shared_prefix_workspace_bytes(const dp_paged_cache *cache, const dp_shared_prefix *prefix) {
-  return paged_ok(cache) == DP_OK && prefix_ok(cache, prefix) ? 256 : 0;
+  if (paged_ok(cache) != DP_OK || !prefix_ok(cache, prefix)) return 0;
+  return align_up(sizeof(float) * dp::paged_partials(view_of(cache), view_of(prefix)), 256);
 }
 
 dp_status dp_shared_prefix_decode(const dp_paged_cache *cache, const dp_shared_prefix *prefix, const void *q, void *out,
@@ -748,10 +765,8 @@ dp_status dp_shared_prefix_decode(const dp_paged_cache *cache, const dp_shared_p
   if (!q || !aligned16(q) || !out || !workspace) return DP_ERR_INVALID_ARG;
   if (workspace_bytes < dp_shared_prefix_workspace_bytes(cache, prefix)) return DP_ERR_WORKSPACE_TOO_SMALL;
   if (reinterpret_cast<uintptr_t>(workspace) % 256) return DP_ERR_INVALID_ARG;
-  const dp::PagedAttention a{q, nullptr, nullptr, nullptr};
-  const dp::AttnOut attn{out, lse, out_dtype == DP_BF16};
-  return dp::launch_paged_decode(view_of(cache), a, attn, static_cast<hipStream_t>(stream)) == hipSuccess ? DP_OK
-                                                                                                         : DP_ERR_HIP;
+  return paged_attention(cache, dp::PagedAttention{q, nullptr, nullptr, nullptr, view_of(prefix)}, out, out_dtype, lse,
+                         workspace, stream);
 }
 
 const char *dp_status_string(dp_status status) {

@@ -152,12 +152,23 @@ struct AppendTokens {
 };
 hipError_t launch_append(const PagedView &c, const AppendTokens &t, hipStream_t s);
 
+// Groups of sequences that begin with the same rows; n_groups == 0: none
+struct SharedView {
+  int32_t n_groups, max_group_seqs, max_shared_len;
+  const int32_t *group_ptr, *shared_lens;
+};
+
+// Rows of a paged cache are attended in pieces whose partial results (max, sum, acc[128]) are merged by a second kernel.
 struct PagedAttention {
   const void *q;
-  const int32_t *first_rows;              // nullable
-  const float *prior_out, *prior_lse;     // nullable
+  const int32_t *first_rows;           // nullable; not with shared rows
+  const float *prior_out, *prior_lse;  // nullable; not with shared rows
+  SharedView shared;
 };
-hipError_t launch_paged_decode(const PagedView &c, const PagedAttention &a, const AttnOut &attn, hipStream_t s);
+// floats of workspace
+size_t paged_partials(const PagedView &c, const SharedView &shared);
+hipError_t launch_paged_decode(const PagedView &c, const PagedAttention &a, float *partials, const AttnOut &attn,
+                               hipStream_t s);
 
 // Prefill side: token-order K / V + cluster ids -> cluster-contiguous cache and cluster metadata.
 struct BuildProblem {

@@ -54,6 +54,8 @@ BAD_CACHES = [
     (UNSUPPORTED, dict(head_dim=64)), (UNSUPPORTED, dict(page_size=24)), (UNSUPPORTED, dict(page_size=48)),
     (UNSUPPORTED, dict(n_seqs=1 << 22)), (UNSUPPORTED, dict(n_seqs=(1 << 31) - 1)),
     (UNSUPPORTED, dict(slot_stride=1 << 30)), (UNSUPPORTED, dict(slot_stride=1 << 62)),
+    (UNSUPPORTED, dict(max_seq_len=(1 << 30) + 1, table_stride=1 << 27)),
+    (UNSUPPORTED, dict(n_seqs=1 << 14, max_seq_len=1 << 22, table_stride=1 << 18)),
     (UNSUPPORTED, dict(page_stride=1 << 60)), (UNSUPPORTED, dict(head_stride=1 << 60)),
 ]
 
