@@ -282,7 +282,7 @@ dp_status paged_ok(const dp_paged_cache *c) {
     return DP_ERR_INVALID_ARG;
   if (c->head_dim != dp::kHeadDim || (c->page_size & (c->page_size - 1)) ||
       (int64_t)c->n_seqs * c->n_q_heads > kMaxPagedHeads || c->max_seq_len > kMaxPagedLen ||
-      (int64_t)c->n_seqs * c->n_kv_heads * (c->max_seq_len / dp::kChunkRows + 1) >= (int64_t)1 << 30)
+      (int64_t)c->n_seqs * c->n_q_heads * (c->max_seq_len / dp::kChunkRows + 1) >= (int64_t)1 << 31)
     return DP_ERR_UNSUPPORTED;
   // the places of a pool fit 64 bits, those of a head's rows inside a page 31
   constexpr int64_t kMost = (int64_t)1 << 58;

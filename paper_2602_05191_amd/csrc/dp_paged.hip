@@ -32,18 +32,27 @@ constexpr int kPagedThreads = 256;
 constexpr int kPagedWaves = kPagedThreads / 64;
 constexpr int kPagedHeads = 16;  // query heads per pass: the columns of one MFMA tile
 constexpr int kPagedTile = 16;   // rows per wave and step
-constexpr int kPartialStride = kHeadDim + 2;
-constexpr int kDealtSeqs = 64 * 64;  // most sequences that the lookup can hold
+constexpr int kDealtItems = 64 * 64;  // most sequences, or groups, that the lookup of a share can hold
+
+// Partial results of a head: per slot the accumulator of its 128 dimensions, (maximum in base 2, sum).  The slots of its
+// own rows come first, then those of the rows that it shares.
+struct Partials {
+  float *acc;
+  float2 *ml;
+  int32_t own, all;  // slots per head
+};
 
 struct PagedArgs {
   PagedView c;
   PagedAttention a;
   AttnOut attn;
-  float *partials;   // [heads, splits, kPartialStride]
-  int32_t head0;     // this launch serves heads [head0, head0 + 16) of every group
-  int32_t splits;    // partial slots per head
-  int32_t min_share, grid;
-  int32_t whole;     // nothing dealt out: a workgroup per segment
+  Partials parts;
+  int32_t head0;        // this launch serves heads [head0, head0 + 16) of every group
+  int32_t whole;        // own rows: nothing dealt out, a workgroup per segment
+  int32_t direct;       // ... which then writes the output itself
+  Deal own, shared;     // shared.slots == 0: no shared rows
+  int32_t shared_cols;  // columns (sequences x query heads of a KV head) per workgroup over shared rows
+  int32_t shared_block; // rows per chunk there
   float scale_log2;
 };
 
@@ -61,70 +70,16 @@ struct SeqRows {
 __device__ __forceinline__ SeqRows seq_rows(const PagedArgs &p, int s) {
   SeqRows r;
   r.len = paged_len(p.c, s);
-  r.first = p.a.first_rows ? max(0, p.a.first_rows[s]) : 0;
+  int group;
+  r.first = p.shared.slots ? shared_rows(p.c, p.a.shared, s, r.len, group) : p.a.first_rows ? max(0, p.a.first_rows[s]) : 0;
   return r;
 }
-
-// The chunks of all segments, numbered through in (sequence, KV head) order: workgroup w takes [w share, (w + 1) share).
-__device__ __forceinline__ int dealt_share(const PagedArgs &p, int total) {
-  return max(p.min_share, (total + p.grid - 1) / p.grid);
-}
-struct PagedStart {
-  int seq, kv, first;    // the segment that holds chunk c, its first chunk's number
-  SeqRows rows;
-  int c, c_end, share;
-};
-// By every wave for itself: a lane adds up `per` consecutive sequences, then the lane that holds the chunk has its
-// sequences spread over the lanes.  false: no chunk is left.
-__device__ __forceinline__ bool paged_start(const PagedArgs &p, PagedStart &d) {
-  const int lane = lane_id(), n = p.c.n_seqs, per = (n + 63) / 64;
-  SeqRows rows{0, 0};
-  auto look = [&](int s, bool valid) {
-    rows = seq_rows(p, min(s, n - 1));
-    return valid && s < n ? rows.chunks() * p.c.n_kv_heads : 0;
+// sequences, and the KV heads of each
+__device__ __forceinline__ auto own_segments(const PagedArgs &p) {
+  return [&p](int s) {
+    const SeqRows r = seq_rows(p, s);
+    return Segments{r.chunks(), p.c.n_kv_heads, r.first, r.len};
   };
-  int mine = 0;
-  if (per == 1) {
-    mine = look(lane, true);
-  } else {
-    for (int u = 0; u < per; ++u) mine += look(lane * per + u, true);
-  }
-  int upto = wave_incl_scan(mine);
-  const int total = (int)lane_u32((uint32_t)upto, 63);
-  d.share = dealt_share(p, total);
-  d.c = blockIdx.x * d.share;
-  d.c_end = min(total, d.c + d.share);
-  if (d.c >= d.c_end) return false;
-  int at = __builtin_ctzll(__ballot(upto - mine <= d.c && d.c < upto));
-  d.seq = at * per;
-  int first = (int)lane_u32((uint32_t)(upto - mine), at);
-  if (per > 1) {
-    mine = look(d.seq + lane, lane < per);
-    upto = first + wave_incl_scan(mine);
-    at = __builtin_ctzll(__ballot(upto - mine <= d.c && d.c < upto));
-    d.seq += at;
-    first = (int)lane_u32((uint32_t)(upto - mine), at);
-  }
-  d.rows.first = (int)lane_u32((uint32_t)rows.first, at);
-  d.rows.len = (int)lane_u32((uint32_t)rows.len, at);
-  d.kv = (d.c - first) / d.rows.chunks();
-  d.first = first + d.kv * d.rows.chunks();
-  return true;
-}
-
-// Number of the first piece of segment (my_seq, kv), which has rows, and how many there are; by every wave for itself.
-__device__ __forceinline__ int paged_pieces(const PagedArgs &p, int my_seq, int kv, int chunks) {
-  int total = 0, before = 0;
-  for (int u = 0; u < p.c.n_seqs; u += 64) {
-    const int s = u + lane_id();
-    const int n = s < p.c.n_seqs ? seq_rows(p, min(s, p.c.n_seqs - 1)).chunks() : 0;
-    total += n;
-    before += s < my_seq ? n : 0;
-  }
-  total = wave_sum(total) * p.c.n_kv_heads;
-  const int first = wave_sum(before) * p.c.n_kv_heads + kv * chunks;
-  const int share = dealt_share(p, total);
-  return (first + chunks - 1) / share - first / share + 1;
 }
 
 // one wave's 16 rows as the two contractions want them, and which of them count
@@ -219,26 +174,26 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
   const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
   const int r = lane & 15, kq = lane >> 4;
   const int n_kv = p.c.n_kv_heads, group = p.c.group, n_live = min(kPagedHeads, group - p.head0);
-  PagedStart at;
+  Dealt at;
   if (p.whole) {
-    at.seq = blockIdx.x / n_kv;
-    at.kv = blockIdx.x % n_kv;
-    at.rows = seq_rows(p, at.seq);
+    at.i = blockIdx.x / n_kv;
+    at.sub = blockIdx.x % n_kv;
+    at.item = own_segments(p)(at.i);
     at.first = at.c = 0;
-    at.c_end = at.rows.chunks();
+    at.c_end = at.item.chunks;
     at.share = 1;
-  } else if (!paged_start(p, at)) {
+  } else if (!deal_start(p.own, p.c.n_seqs, own_segments(p), at)) {
     return;
   }
 
   // one piece of a segment after the other, usually one
   while (true) {
-    const SeqRows rows = at.rows;
-    const int seg_end = at.first + rows.chunks();
+    const SeqRows rows{at.item.a, at.item.b};
+    const int seg_end = at.first + at.item.chunks;
     const int ra = (rows.chunk0() + at.c - at.first) * kChunkRows;
     const int rb = min(rows.len, (rows.chunk0() + min(at.c_end, seg_end) - at.first) * kChunkRows);
-    const int split = blockIdx.x - at.first / at.share;  // number of the piece inside its segment
-    const int64_t head_first = (int64_t)at.seq * p.c.n_q_heads + at.kv * group + p.head0;
+    const int split = p.whole ? 0 : blockIdx.x - at.first / at.share;  // number of the piece inside its segment
+    const int64_t head_first = (int64_t)at.i * p.c.n_q_heads + at.sub * group + p.head0;
 
     // query head r of the pass (beyond the group: its last head again, not stored), chunks kq + 4 j
     uint4 Q[4];
@@ -297,7 +252,7 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
     };
 
     // the workgroup's waves take tiles in turn; the next tile's loads are in flight during a tile's arithmetic
-    TileLoader<kSmallPages> tiles(p.c, at.seq, at.kv, rows);
+    TileLoader<kSmallPages> tiles(p.c, at.i, at.sub, rows);
     constexpr int kStep = TileLoader<kSmallPages>::kStep;
     int t = ra + wave * kPagedTile;
     if (t < rb) {
@@ -341,7 +296,7 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
     constexpr int kMost = kPagedHeads / (kPagedThreads / kHeadDim);
     const int d = tid % kHeadDim, j0 = tid / kHeadDim;
     float prior_o[kMost], prior_lse[kMost];
-    if (p.whole && p.a.prior_lse) {
+    if (p.direct && p.a.prior_lse) {
 #pragma unroll
       for (int u = 0; u < kMost; ++u) {
         const int64_t head = head_first + min(j0 + u * (kPagedThreads / kHeadDim), n_live - 1);
@@ -364,25 +319,270 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
         x.l += s_l[w][j] * wg;
         x.o += s_acc[w][j][d] * wg;
       }
-      if (p.whole) {
+      if (p.direct) {
         store_head(p, head_first + j, d, p.a.prior_lse ? prior_lse[u] : -INFINITY, p.a.prior_lse ? prior_o[u] : 0.f, x);
         continue;
       }
-      float *P = p.partials + ((head_first + j) * p.splits + split) * kPartialStride;
-      if (d == 0) {
-        P[0] = x.m;
-        P[1] = x.l;
-      }
-      P[2 + d] = x.o;
+      const int64_t slot = (head_first + j) * p.parts.all + split;
+      p.parts.acc[slot * kHeadDim + d] = x.o;
+      if (d == 0) p.parts.ml[slot] = make_float2(x.m, x.l);
     }
-    at.c = at.first = seg_end;
-    if (at.c >= at.c_end) break;
+    if (seg_end >= at.c_end) break;
     __syncthreads();  // LDS is reused by the next piece
-    if (++at.kv == n_kv) {
-      at.kv = 0;
-      do at.rows = seq_rows(p, ++at.seq);
-      while (at.rows.chunks() == 0);  // (a sequence with rows follows: chunks are left)
+    deal_next(own_segments(p), at);
+  }
+}
+
+// ---- rows that a group shares ----
+// The columns are the queries of all sequences of the group, G per sequence: with tens of columns and more the products
+// are large enough for the matrix cores' bf16 rate, and the rows are read once for all of them.
+//   scores  S^T[32 rows x 32 columns] = K Q^T, v_mfma_f32_32x32x16_bf16, the keys from LDS, the queries in registers: a
+//           lane holds 16 scores of column lane % 32, rows 8 (i / 4) + 4 (lane / 32) + i % 4;
+//   output  O^T[dims x columns] += V^T P^T, the same instruction: weights i = 8 n .. 8 n + 7 of a lane are the k = 8
+//           (lane / 32) .. + 7 of the n-th 16 rows if the values come in that order of rows, and they do: ds_read_tr16_b64
+//           hands a lane one dimension of four consecutive rows, two of them the eight rows 16 n + 4 (lane / 32) + {0 .. 3,
+//           8 .. 11}.  Nothing moves between lanes but the two halves' maxima.
+// Weights go into the product in bf16 pieces that add up: two (16 bits) for a bf16 output, three (all 24) for fp32; their
+// sum is taken from the fp32 weights.  (One piece rounds a weight by up to 2^-9, as much as the output itself is rounded.)
+// All but the last piece are cut, not rounded, and what is left is increased by 2^-23 (three pieces: 2^-26, 2^-34) of the
+// weight: no piece is zero, so that an infinite value does not become NaN (0 x inf).
+// A weight below 2^-126 of the largest counts as zero here (v_exp_f32).
+// kCols column tiles x kParts parts of a block's rows = the waves of a workgroup.  A block of 64 or 128 rows goes global ->
+// registers -> LDS while the one before is attended; rows padded to 272 (keys) and 288 (values) bytes.
+template <int kCols, int kParts>
+struct SharedShape {
+  static constexpr int kWaves = kCols * kParts, kThreads = 64 * kWaves;
+  static constexpr int kRows = kParts * 32 < 64 ? 64 : kParts * 32;
+  static constexpr int kSubs = kRows / (32 * kParts);  // 32-row tiles of a wave in a block
+  static constexpr int kLoads = kRows * 16 / kThreads;  // 16-byte loads of a thread per block, of keys and of values
+  static constexpr int kBuffers = kWaves == 4 ? 1 : 2;
+  static constexpr int kKPitch = 272, kVPitch = 288;
+  static constexpr int kBuffer = kRows * (kKPitch + kVPitch);
+  static constexpr int kResident = kWaves == 4 ? 512 : 256;  // two waves per SIMD
+};
+
+// groups; their KV heads, and of each the column tiles of a workgroup
+__device__ __forceinline__ auto shared_segments(const PagedArgs &p) {
+  return [&p](int g) {
+    const SharedGroup s = shared_group(p.c, p.a.shared, g);
+    const int tiles = ((s.end - s.begin) * p.c.group + p.shared_cols - 1) / p.shared_cols;
+    return Segments{(s.rows + p.shared_block - 1) / p.shared_block, p.c.n_kv_heads * tiles, s.begin, s.reader};
+  };
+}
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 *LdsTile;
+
+template <int kCols, int kParts, int kPieces>
+__global__ __launch_bounds__(64 * kCols *kParts)
+    __attribute__((amdgpu_waves_per_eu(2, 2))) void shared_kernel(PagedArgs p) {
+  using S = SharedShape<kCols, kParts>;
+  __shared__ __align__(16) char s_rows[S::kBuffers][S::kBuffer];
+  const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
+  const int col_tile = wave % kCols, part = wave / kCols, half = lane >> 5;
+  const PagedView &c = p.c;
+  Dealt at;
+  if (!deal_start(p.shared, p.a.shared.n_groups, shared_segments(p), at)) return;
+
+  while (true) {
+    const SharedGroup grp = shared_group(c, p.a.shared, at.i);
+    const int tiles = at.item.subs / c.n_kv_heads, kv = at.sub / tiles, col0 = at.sub % tiles * p.shared_cols + 32 * col_tile;
+    const int n_cols = (grp.end - grp.begin) * c.group;
+    const int split = blockIdx.x - at.first / at.share, seg_end = at.first + at.item.chunks;
+    const int block0 = at.c - at.first, block1 = min(at.c_end, seg_end) - at.first;
+    const int32_t *table = c.table + (int64_t)grp.reader * c.table_stride;
+    const bool busy = col0 < n_cols;
+
+    // the lane's column: a query head of one of the sequences
+    const int col = min(col0 + (lane & 31), n_cols - 1), col_seq = grp.begin + col / c.group;
+    const int64_t head = (int64_t)col_seq * c.n_q_heads + kv * c.group + col % c.group;
+    const bool mine = col0 + (lane & 31) < n_cols && paged_len(c, col_seq) >= grp.rows;
+    uint4 Q[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      Q[k] = *reinterpret_cast<const uint4 *>(static_cast<const char *>(p.a.q) + head * kRowBytes + k * 32 + half * 16);
+    f32x16 O[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) O[n][i] = 0.f;
+    float m = -INFINITY, l = 0.f;
+
+    // ---- a block's rows: 16 lanes per row, kLoads rows per thread; pages looked up a block ahead ----
+    constexpr int kRowsPerLoad = S::kThreads / 16;
+    const char *k_head = c.k_pages + kv * c.head_stride + (tid & 15) * 16, *v_head = c.v_pages + kv * c.head_stride + (tid & 15) * 16;
+    int pages[S::kLoads], live_page[S::kSubs];
+    uint4 kr[S::kLoads], vr[S::kLoads];
+    uint32_t live[S::kSubs], live_next[S::kSubs], here = 0;  // here: bit i for the row of load i
+    auto page_of = [&](int row) { return row < grp.rows ? table[row >> c.page_shift] : -1; };
+    auto look_up = [&](int block) {
+#pragma unroll
+      for (int i = 0; i < S::kLoads; ++i) pages[i] = page_of(block * S::kRows + i * kRowsPerLoad + (tid >> 4));
+#pragma unroll
+      for (int u = 0; u < S::kSubs; ++u) live_page[u] = page_of(block * S::kRows + (u * kParts + part) * 32 + (lane & 31));
+    };
+    auto fetch = [&](int block) {
+      here = 0;
+#pragma unroll
+      for (int i = 0; i < S::kLoads; ++i) {
+        const int row = block * S::kRows + i * kRowsPerLoad + (tid >> 4);
+        const bool there = (uint32_t)pages[i] < (uint32_t)c.n_pages;
+        const int64_t place = (there ? pages[i] : 0) * c.page_stride + (row & ((1 << c.page_shift) - 1)) * (int64_t)c.slot_stride;
+        kr[i] = load_stream16(k_head + place);
+        vr[i] = load_stream16(v_head + place);
+        here |= (uint32_t)there << i;
+      }
+#pragma unroll
+      for (int u = 0; u < S::kSubs; ++u)
+        live_next[u] = (uint32_t)__ballot((uint32_t)live_page[u] < (uint32_t)c.n_pages);
+    };
+    auto put = [&](char *buffer) {  // (values of rows that are not there: zero)
+#pragma unroll
+      for (int i = 0; i < S::kLoads; ++i) {
+        const int row = i * kRowsPerLoad + (tid >> 4);
+        *reinterpret_cast<uint4 *>(buffer + row * S::kKPitch + (tid & 15) * 16) = kr[i];
+        *reinterpret_cast<uint4 *>(buffer + S::kRows * S::kKPitch + row * S::kVPitch + (tid & 15) * 16) =
+            here >> i & 1 ? vr[i] : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int u = 0; u < S::kSubs; ++u) live[u] = live_next[u];
+    };
+
+    auto attend = [&](const char *buffer) {
+#pragma unroll
+      for (int u = 0; u < S::kSubs; ++u) {
+        if (live[u] == 0) continue;
+        const int row0 = (u * kParts + part) * 32;
+        const char *k = buffer + (row0 + (lane & 31)) * S::kKPitch + half * 16;
+        f32x16 x;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(k + 32 * j)),
+                                                      __builtin_bit_cast(bf16x8, Q[j]), x, 0, 0, 0);
+        if (live[u] != 0xffffffffu) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            x[i] = (live[u] >> (8 * (i / 4) + 4 * half + i % 4)) & 1 ? x[i] : -INFINITY;
+        }
+        float top = x[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+        top = fmaxf(m, fmaxf(top, xor32(top)));
+        if (__ballot(top > m)) {
+          const float alpha = __builtin_amdgcn_exp2f((m - finite_max(top)) * p.scale_log2);
+          l *= alpha;
+#pragma unroll
+          for (int n = 0; n < 4; ++n) O[n] *= alpha;
+          m = top;
+        }
+        const float sub = finite_max(m);
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          x[i] = __builtin_amdgcn_exp2f((x[i] - sub) * p.scale_log2);
+          sum += x[i];
+        }
+        l += sum;
+        // the value rows 4 half + (lane % 16) / 4 of a quad, dims 16 (lane / 16 % 2) + 4 (lane % 4)
+        const char *v = buffer + S::kRows * S::kKPitch + (row0 + 4 * half + (lane & 15) / 4) * S::kVPitch +
+                        (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          float w[8], rest[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[e] = rest[e] = x[8 * n + e];
+          bf16x8 piece[kPieces];
+#pragma unroll
+          for (int q = 0; q < kPieces; ++q) {
+            if (q + 1 < kPieces) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const float cut = __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
+                piece[q][e] = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(rest[e]) >> 16));
+                rest[e] = fmaf(w[e], kPieces == 2 ? 0x1p-23f : q == 0 ? 0x1p-26f : 0x1p-34f, rest[e] - cut);
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) piece[q][e] = (__bf16)rest[e];
+            }
+          }
+#pragma unroll
+          for (int dt = 0; dt < 4; ++dt) {
+            const char *at = v + n * 16 * S::kVPitch + dt * 64;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsTile)(at));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsTile)(at + 8 * S::kVPitch));
+            const bf16x8 values = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int q = 0; q < kPieces; ++q)
+              O[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values, piece[q], O[dt], 0, 0, 0);
+          }
+        }
+      }
+    };
+
+    look_up(block0);
+    fetch(block0);
+    look_up(block0 + 1);
+    put(s_rows[0]);
+    __syncthreads();
+    for (int b = block0; b < block1; ++b) {
+      const int now = S::kBuffers == 1 ? 0 : (b - block0) & 1;
+      if (b + 1 < block1) {
+        fetch(b + 1);
+        look_up(b + 2);
+        if (busy) attend(s_rows[now]);
+        if constexpr (S::kBuffers == 1) __syncthreads();
+        put(s_rows[S::kBuffers == 1 ? 0 : now ^ 1]);
+      } else if (busy) {
+        attend(s_rows[now]);
+      }
+      __syncthreads();
     }
+    l += xor32(l);
+
+    // the parts of the rows meet in LDS, in pairs
+    m *= p.scale_log2;
+    float *meet = reinterpret_cast<float *>(&s_rows[0][0]);
+    static_assert(kParts == 1 || (kCols * kParts / 2) * 66 * 64 * 4 <= S::kBuffers * S::kBuffer, "the halves fit the buffers");
+#pragma unroll
+    for (int step = kParts / 2; step > 0; step /= 2) {
+      float *slot = meet + (part % step * kCols + col_tile) * 66 * 64 + lane;
+      if (part >= step && part < 2 * step) {
+        slot[64 * 64] = m;
+        slot[65 * 64] = l;
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) slot[(16 * n + i) * 64] = O[n][i];
+      }
+      __syncthreads();
+      if (part < step) {
+        const float mo = slot[64 * 64], top = fmaxf(m, mo), sub = finite_max(top);
+        const float w = __builtin_amdgcn_exp2f(m - sub), wo = __builtin_amdgcn_exp2f(mo - sub);
+        l = fmaf(l, w, slot[65 * 64] * wo);
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) O[n][i] = fmaf(O[n][i], w, slot[(16 * n + i) * 64] * wo);
+        m = top;
+      }
+      __syncthreads();
+    }
+
+    if (busy && mine && part == 0) {
+      const int64_t slot = head * p.parts.all + p.parts.own + split;
+      if (half == 0) p.parts.ml[slot] = make_float2(m, l);
+      float4 *dst = reinterpret_cast<float4 *>(p.parts.acc + slot * kHeadDim + 4 * half);
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dst[8 * n + 2 * i] = make_float4(O[n][4 * i], O[n][4 * i + 1], O[n][4 * i + 2], O[n][4 * i + 3]);
+    }
+    if (seg_end >= at.c_end) break;
+    deal_next(shared_segments(p), at);
   }
 }
 
@@ -393,21 +593,33 @@ __global__ __launch_bounds__(kGroups * kHeadDim) void paged_merge_kernel(PagedAr
   __shared__ float s_m[kGroups], s_l[kGroups], s_o[kGroups][kHeadDim];
   const int head = blockIdx.x, t = threadIdx.x % kHeadDim, grp = threadIdx.x / kHeadDim;
   const int seq = head / p.c.n_q_heads, kv = head % p.c.n_q_heads / p.c.group;
-  const int chunks = seq_rows(p, seq).chunks();
-  const int n_active = chunks ? paged_pieces(p, seq, kv, chunks) : 0;
+  const SeqRows rows = seq_rows(p, seq);
+  const int chunks = rows.chunks();
+  const int n_own = p.whole ? 1 : chunks ? deal_pieces(p.own, p.c.n_seqs, own_segments(p), seq, kv, chunks) : 0;
+  int n_active = n_own;
+  if (p.shared.slots && rows.first > 0) {
+    int g;
+    shared_rows(p.c, p.a.shared, seq, rows.len, g);
+    const Segments s = shared_segments(p)(g);
+    const int column = (seq - s.a) * p.c.group + head % p.c.group;
+    n_active += deal_pieces(p.shared, p.a.shared.n_groups, shared_segments(p), g,
+                            kv * (s.subs / p.c.n_kv_heads) + column / p.shared_cols, s.chunks);
+  }
   const float prior_lse = p.a.prior_lse ? p.a.prior_lse[head] : -INFINITY;
   const float prior_o = p.a.prior_lse ? p.a.prior_out[(int64_t)head * kHeadDim + t] : 0.f;
-  const float *P = p.partials + (int64_t)head * p.splits * kPartialStride;
+  const int64_t slot0 = (int64_t)head * p.parts.all;
   constexpr int kBatch = 8;
   Merged x{-INFINITY, 0.f, 0.f};
   for (int s0 = grp; s0 < n_active; s0 += kGroups * kBatch) {
     float ms[kBatch], ll[kBatch], oo[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      const float *Q = P + min(s0 + kGroups * u, n_active - 1) * kPartialStride;
-      ms[u] = Q[0];
-      ll[u] = Q[1];
-      oo[u] = Q[2 + t];
+      int s = min(s0 + kGroups * u, n_active - 1);
+      s = s < n_own ? s : s - n_own + p.parts.own;
+      const float2 ml = p.parts.ml[slot0 + s];
+      ms[u] = ml.x;
+      ll[u] = ml.y;
+      oo[u] = p.parts.acc[(slot0 + s) * kHeadDim + t];
     }
     float Mn = x.m;
 #pragma unroll
@@ -450,47 +662,83 @@ __global__ __launch_bounds__(kGroups * kHeadDim) void paged_merge_kernel(PagedAr
 
 // How a call is split; by sizes that the host knows.
 struct Split {
-  int whole, splits, min_share, grid;
+  int whole, cols, parts;  // own rows; shared rows: the shape of a workgroup
+  Deal own, shared;
+  int shared_block;
 };
-Split split_of(const PagedView &c) {
-  Split s;
+int at_most(long n, long most) { return (int)(n < most ? n : most); }
+int at_least(long n, long least) { return (int)(n > least ? n : least); }
+
+Split split_of(const PagedView &c, const SharedView &shared) {
+  Split s{};
   const long n_seg = (long)c.n_seqs * c.n_kv_heads, nh = (long)c.n_seqs * c.n_q_heads;
   const int max_chunks = (c.max_seq_len + kChunkRows - 1) / kChunkRows;
-  s.whole = c.n_seqs > kDealtSeqs || c.max_seq_len <= (n_seg >= 512 ? 1024 : n_seg >= 128 ? 512 : 320);
-  // partial slots per head: some thousand pieces in all, never more than a head has chunks
-  long slots = 16384 / nh;
-  slots = slots < 8 ? 8 : slots > kMaxSplits ? kMaxSplits : slots;
-  s.splits = (int)(slots < max_chunks ? slots : max_chunks > 0 ? max_chunks : 1);
-  // A segment of n chunks has at most ceil(n / share) + 1 pieces, and never more than n: the share is large enough for
-  // the partial slots of a head.  One round of workgroups: two waves per SIMD x 256 CUs.
-  s.min_share = 1;
-  if (max_chunks > s.splits && s.splits > 1) s.min_share = (max_chunks + s.splits - 2) / (s.splits - 1);
-  constexpr int kResident = 2 * 256;
-  const long want = (n_seg * max_chunks + s.min_share - 1) / s.min_share;
-  s.grid = (int)(want < 1 ? 1 : want < kResident ? want : kResident);
+  s.whole = c.n_seqs > kDealtItems || c.max_seq_len <= (n_seg >= 512 ? 1024 : n_seg >= 128 ? 512 : 320);
+  // one round of workgroups (two waves per SIMD x 256 CUs), and partial slots for some thousand pieces in all
+  s.own.grid = at_least(at_most(n_seg * max_chunks, 2 * 256), 1);
+  s.own.slots = s.whole ? 1 : at_least(at_most(max_chunks, at_most(at_least(16384 / nh, 8), kMaxSplits)), 1);
+  if (shared.n_groups == 0 || shared.max_shared_len == 0 || shared.n_groups > kDealtItems) return s;
+  const long cols = (long)(shared.max_group_seqs < c.n_seqs ? shared.max_group_seqs : c.n_seqs) * c.group;
+  s.cols = cols <= 32 ? 1 : cols <= 64 ? 2 : cols <= 128 ? 4 : 8;
+  s.parts = s.cols == 1 ? 4 : 8 / s.cols;
+  s.shared_block = s.parts * 32 < 64 ? 64 : s.parts * 32;
+  s.shared.grid = s.cols == 1 ? 512 : 256;
+  // a segment has at most ceil(grid / KV heads) + 1 pieces
+  const int max_blocks = (shared.max_shared_len + s.shared_block - 1) / s.shared_block;
+  s.shared.slots = at_most(at_most(max_blocks, s.shared.grid / c.n_kv_heads + 2), at_least(131072 / nh, 8));
   return s;
+}
+
+template <int kCols, int kParts>
+void launch_shared(const PagedArgs &p, hipStream_t stream) {
+  using S = SharedShape<kCols, kParts>;
+  if (p.attn.out_is_bf16)
+    hipLaunchKernelGGL((shared_kernel<kCols, kParts, 2>), dim3(p.shared.grid), dim3(S::kThreads), 0, stream, p);
+  else
+    hipLaunchKernelGGL((shared_kernel<kCols, kParts, 3>), dim3(p.shared.grid), dim3(S::kThreads), 0, stream, p);
 }
 
 }  // namespace
 
-size_t paged_partials(const PagedView &c, const SharedView &) {
-  const Split s = split_of(c);
-  return s.whole ? 1 : (size_t)c.n_seqs * c.n_q_heads * s.splits * kPartialStride;
+size_t paged_partials(const PagedView &c, const SharedView &shared) {
+  const Split s = split_of(c, shared);
+  const size_t slots = s.whole && !s.shared.slots ? 0 : (size_t)s.own.slots + s.shared.slots;
+  return (size_t)c.n_seqs * c.n_q_heads * slots * (kHeadDim + 2) + 1;
 }
 
 hipError_t launch_paged_decode(const PagedView &c, const PagedAttention &a, float *partials, const AttnOut &attn,
                                hipStream_t stream) {
-  const Split s = split_of(c);
-  PagedArgs p{c, a, attn, partials, 0, s.splits, s.min_share, s.grid, s.whole, c.sm_scale * kLog2e};
+  const Split s = split_of(c, a.shared);
   const int nh = c.n_seqs * c.n_q_heads;
-  const dim3 grid(s.whole ? c.n_seqs * c.n_kv_heads : s.grid), block(kPagedThreads);
+  PagedArgs p{};
+  p.c = c;
+  p.a = a;
+  p.attn = attn;
+  p.parts.own = s.own.slots;
+  p.parts.all = s.own.slots + s.shared.slots;
+  p.parts.acc = partials;
+  p.parts.ml = reinterpret_cast<float2 *>(partials + (size_t)nh * p.parts.all * kHeadDim);
+  p.whole = s.whole;
+  p.direct = s.whole && !s.shared.slots;
+  p.own = s.own;
+  p.shared = s.shared;
+  p.shared_cols = 32 * s.cols;
+  p.shared_block = s.shared_block;
+  p.scale_log2 = c.sm_scale * kLog2e;
+  switch (s.cols) {
+    case 1: launch_shared<1, 4>(p, stream); break;
+    case 2: launch_shared<2, 4>(p, stream); break;
+    case 4: launch_shared<4, 2>(p, stream); break;
+    case 8: launch_shared<8, 1>(p, stream); break;
+  }
+  const dim3 grid(s.whole ? c.n_seqs * c.n_kv_heads : s.own.grid), block(kPagedThreads);
   for (p.head0 = 0; p.head0 < c.group; p.head0 += kPagedHeads) {  // one pass over the rows for up to 16 heads of a group
     if (c.page_shift < 4)
       hipLaunchKernelGGL(paged_kernel<true>, grid, block, 0, stream, p);
     else
       hipLaunchKernelGGL(paged_kernel<false>, grid, block, 0, stream, p);
   }
-  if (s.whole) return hipGetLastError();
+  if (p.direct) return hipGetLastError();
   if (nh >= 512 || c.max_seq_len <= 32 * kChunkRows)
     hipLaunchKernelGGL(paged_merge_kernel<1>, dim3(nh), dim3(kHeadDim), 0, stream, p);
   else

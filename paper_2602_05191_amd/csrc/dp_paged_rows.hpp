@@ -33,12 +33,113 @@ __device__ __forceinline__ int lane_find(const int32_t *ptr, int n, int x) {
 
 __device__ __forceinline__ int paged_len(const PagedView &c, int s) { return max(0, min(c.seq_lens[s], c.max_seq_len)); }
 
-// Rows that sequence s shares with its group (0: none; a sequence that is too short for them shares none).
-__device__ __forceinline__ int shared_rows(const SharedView &p, int s, int len) {
-  const int g = lane_find(p.group_ptr, p.n_groups, s);
-  if (g >= p.n_groups || s - p.group_ptr[g] >= p.max_group_seqs) return 0;
-  const int n = max(0, min(p.shared_lens[g], p.max_shared_len));
+// The sequences [begin, end) of group g that share rows, what they share (0 where none is long enough to hold it) and the
+// first of them that holds it, through whose table the rows are read.
+struct SharedGroup {
+  int begin, end, rows, reader;
+};
+__device__ __forceinline__ SharedGroup shared_group(const PagedView &c, const SharedView &p, int g) {
+  SharedGroup s;
+  s.begin = max(0, min(p.group_ptr[g], c.n_seqs));
+  s.end = max(s.begin, min(p.group_ptr[g + 1], c.n_seqs));
+  s.end = s.begin + min(s.end - s.begin, p.max_group_seqs);
+  s.rows = max(0, min(p.shared_lens[g], p.max_shared_len));
+  s.reader = s.begin;
+  while (s.reader < s.end && paged_len(c, s.reader) < s.rows) ++s.reader;
+  if (s.reader == s.end) s.rows = 0;
+  return s;
+}
+// The group of sequence s (n_groups: none) and the rows that s shares (0: none; too short a sequence shares none).
+__device__ __forceinline__ int shared_rows(const PagedView &c, const SharedView &p, int s, int len, int &group) {
+  group = lane_find(p.group_ptr, p.n_groups, s);
+  if (group >= p.n_groups || s - max(0, p.group_ptr[group]) >= p.max_group_seqs) return 0;
+  const int n = max(0, min(p.shared_lens[group], p.max_shared_len));
   return n <= len ? n : 0;
+}
+
+// ---- work dealt out evenly ----
+// n items; item i is subs segments of chunks chunks each, all numbered through in this order.  One round of workgroups
+// takes equal shares: workgroup w chunks [w share, (w + 1) share).  A share may end one segment and begin the next, and a
+// segment is cut into at most `slots` pieces: ceil(chunks / share) + 1, or as many as it has chunks.
+struct Segments {
+  int chunks, subs;
+  int a, b;  // what the caller wants to know of the item
+};
+struct Deal {
+  int grid, slots;
+  __device__ __forceinline__ int share(int total, int longest) const {
+    const int least = slots > 1 ? (longest + slots - 2) / (slots - 1) : longest;
+    return max(max(1, longest > slots ? least : 1), (total + grid - 1) / grid);
+  }
+};
+struct Dealt {
+  Segments item;
+  int i, sub, first;      // the segment that holds chunk c, its first chunk's number
+  int c, c_end, share;
+};
+// By every wave for itself: a lane adds up `per` consecutive items, then the lane that holds chunk c has its items spread
+// over the lanes.  n <= 64 * 64.  false: no chunk is left.
+template <class At>
+__device__ __forceinline__ bool deal_start(const Deal &deal, int n, At at, Dealt &d) {
+  const int lane = lane_id(), per = (n + 63) / 64;
+  Segments item{0, 0, 0, 0};
+  auto look = [&](int i, bool valid) {
+    item = at(min(i, n - 1));
+    if (!valid || i >= n) item.chunks = 0;
+    return item.chunks * item.subs;
+  };
+  int mine = 0, longest = 0;
+  for (int u = 0; u < per; ++u) {
+    mine += look(lane * per + u, true);
+    longest = max(longest, item.chunks);
+  }
+  int upto = wave_incl_scan(mine);
+  const int total = (int)lane_u32((uint32_t)upto, 63);
+  d.share = deal.share(total, (int)wave_max((unsigned long long)longest));
+  d.c = blockIdx.x * d.share;
+  d.c_end = min(total, d.c + d.share);
+  if (d.c >= d.c_end) return false;
+  int l = __builtin_ctzll(__ballot(upto - mine <= d.c && d.c < upto));
+  d.i = l * per;
+  int first = (int)lane_u32((uint32_t)(upto - mine), l);
+  if (per > 1) {
+    mine = look(d.i + lane, lane < per);
+    upto = first + wave_incl_scan(mine);
+    l = __builtin_ctzll(__ballot(upto - mine <= d.c && d.c < upto));
+    d.i += l;
+    first = (int)lane_u32((uint32_t)(upto - mine), l);
+  }
+  d.item.chunks = (int)lane_u32((uint32_t)item.chunks, l);
+  d.item.subs = (int)lane_u32((uint32_t)item.subs, l);
+  d.item.a = (int)lane_u32((uint32_t)item.a, l);
+  d.item.b = (int)lane_u32((uint32_t)item.b, l);
+  d.sub = (d.c - first) / d.item.chunks;
+  d.first = first + d.sub * d.item.chunks;
+  return true;
+}
+// To the segment behind the one just done (the caller has checked that chunks are left).
+template <class At>
+__device__ __forceinline__ void deal_next(At at, Dealt &d) {
+  d.c = d.first = d.first + d.item.chunks;
+  if (++d.sub < d.item.subs) return;
+  d.sub = 0;
+  do d.item = at(++d.i);
+  while (d.item.chunks * d.item.subs == 0);
+}
+// Number of pieces of segment (i, sub) of `chunks` chunks, by every wave for itself.
+template <class At>
+__device__ __forceinline__ int deal_pieces(const Deal &deal, int n, At at, int i, int sub, int chunks) {
+  int total = 0, before = 0, longest = 0;
+  for (int u = 0; u < n; u += 64) {
+    const Segments s = at(min(u + lane_id(), n - 1));
+    const int all = u + lane_id() < n ? s.chunks * s.subs : 0;
+    total += all;
+    before += u + lane_id() < i ? all : 0;
+    longest = max(longest, s.chunks);
+  }
+  const int first = wave_sum(before) + sub * chunks;
+  const int share = deal.share(wave_sum(total), (int)wave_max((unsigned long long)longest));
+  return (first + chunks - 1) / share - first / share + 1;
 }
 
 }  // namespace dp

@@ -414,8 +414,10 @@ def test_shared_prefix_is_the_paged_decode(dp):
     P.check(shared_decode(dp, pool, q, ptr, shared, longest=90), ref)
     P.check(shared_decode(dp, pool, q, ptr, shared, longest=0), ref)
     P.check(shared_decode(dp, pool, q, ptr, [-4, 100], longest=300), ref)
-    P.check(shared_decode(dp, pool, q, [2, 6, 40], shared, most=9), ref)     # a group that ends behind the last sequence
-    P.check(shared_decode(dp, pool, q, [-3, 2, 2], [16, 16], most=9), ref)   # ... and one that begins before the first
+    # a group that ends behind the last sequence, one that begins before the first
+    pool = shared_pool([0, 3, 9], [40, 100], own[:9], 2, 16, seed=25)
+    q = queries(pool.rng, 9, 8)
+    P.check(shared_decode(dp, pool, q, [-3, 3, 40], [40, 100], most=9), P.decode(pool, q))
 
 
 def test_shared_prefix_without_rows(dp):
