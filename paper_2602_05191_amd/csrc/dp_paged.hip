@@ -449,77 +449,83 @@ __global__ __launch_bounds__(64 * kCols *kParts)
       for (int u = 0; u < S::kSubs; ++u) live[u] = live_next[u];
     };
 
-    auto attend = [&](const char *buffer) {
+    // one 32-row tile of a block
+    auto attend = [&](const char *buffer, int row0, uint32_t live) {
+      const char *k = buffer + (row0 + (lane & 31)) * S::kKPitch + half * 16;
+      uint4 key[8];
 #pragma unroll
-      for (int u = 0; u < S::kSubs; ++u) {
-        if (live[u] == 0) continue;
-        const int row0 = (u * kParts + part) * 32;
-        const char *k = buffer + (row0 + (lane & 31)) * S::kKPitch + half * 16;
-        f32x16 x;
+      for (int j = 0; j < 8; ++j) key[j] = *reinterpret_cast<const uint4 *>(k + 32 * j);
+      f32x16 x;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = 0.f;
+      for (int i = 0; i < 16; ++i) x[i] = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(k + 32 * j)),
-                                                      __builtin_bit_cast(bf16x8, Q[j]), x, 0, 0, 0);
-        if (live[u] != 0xffffffffu) {
+      for (int j = 0; j < 8; ++j)
+        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, key[j]), __builtin_bit_cast(bf16x8, Q[j]), x,
+                                                    0, 0, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);  // (all reads, then the products)
+      __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+      if (live != 0xffffffffu) {
+        const uint32_t on = live >> (4 * half);
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            x[i] = (live[u] >> (8 * (i / 4) + 4 * half + i % 4)) & 1 ? x[i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) x[i] = on & 1u << (8 * (i / 4) + i % 4) ? x[i] : -INFINITY;
+      }
+      float top = x[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+      top = fmaxf(m, fmaxf(top, xor32(top)));
+      if (top > m) {
+        const float alpha = __builtin_amdgcn_exp2f((m - finite_max(top)) * p.scale_log2);
+        l *= alpha;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) O[n] *= alpha;
+        m = top;
+      }
+      const float sub = finite_max(m);
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        x[i] = __builtin_amdgcn_exp2f((x[i] - sub) * p.scale_log2);
+        sum += x[i];
+      }
+      l += sum;
+      // the value rows 4 half + (lane % 16) / 4 of a quad, dims 16 (lane / 16 % 2) + 4 (lane % 4)
+      const char *v = buffer + S::kRows * S::kKPitch + (row0 + 4 * half + (lane & 15) / 4) * S::kVPitch +
+                      (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+      bf16x8 values[2][4];
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) {
+          const char *at = v + n * 16 * S::kVPitch + dt * 64;
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsTile)(at));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsTile)(at + 8 * S::kVPitch));
+          values[n][dt] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         }
-        float top = x[0];
+      __builtin_amdgcn_sched_group_barrier(0x100, 16, 0);  // (the reads are on their way during the exponentials)
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-        top = fmaxf(m, fmaxf(top, xor32(top)));
-        if (__ballot(top > m)) {
-          const float alpha = __builtin_amdgcn_exp2f((m - finite_max(top)) * p.scale_log2);
-          l *= alpha;
+      for (int n = 0; n < 2; ++n) {
+        float rest[8];
 #pragma unroll
-          for (int n = 0; n < 4; ++n) O[n] *= alpha;
-          m = top;
-        }
-        const float sub = finite_max(m);
-        float sum = 0.f;
+        for (int e = 0; e < 8; ++e) rest[e] = x[8 * n + e];
+        bf16x8 piece[kPieces];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          x[i] = __builtin_amdgcn_exp2f((x[i] - sub) * p.scale_log2);
-          sum += x[i];
-        }
-        l += sum;
-        // the value rows 4 half + (lane % 16) / 4 of a quad, dims 16 (lane / 16 % 2) + 4 (lane % 4)
-        const char *v = buffer + S::kRows * S::kKPitch + (row0 + 4 * half + (lane & 15) / 4) * S::kVPitch +
-                        (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+        for (int q = 0; q + 1 < kPieces; ++q)
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          float w[8], rest[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = rest[e] = x[8 * n + e];
-          bf16x8 piece[kPieces];
-#pragma unroll
-          for (int q = 0; q < kPieces; ++q) {
-            if (q + 1 < kPieces) {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const float cut = __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
-                piece[q][e] = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(rest[e]) >> 16));
-                rest[e] = fmaf(w[e], kPieces == 2 ? 0x1p-23f : q == 0 ? 0x1p-26f : 0x1p-34f, rest[e] - cut);
-              }
-            } else {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) piece[q][e] = (__bf16)rest[e];
-            }
+          for (int e = 0; e < 8; ++e) {
+            const float cut = __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
+            piece[q][e] = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(rest[e]) >> 16));
+            if (kPieces == 2)
+              rest[e] = fmaf(rest[e], 1.f + 0x1p-23f, -cut);
+            else
+              rest[e] = fmaf(x[8 * n + e], q == 0 ? 0x1p-26f : 0x1p-34f, rest[e] - cut);
           }
 #pragma unroll
-          for (int dt = 0; dt < 4; ++dt) {
-            const char *at = v + n * 16 * S::kVPitch + dt * 64;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsTile)(at));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsTile)(at + 8 * S::kVPitch));
-            const bf16x8 values = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        for (int e = 0; e < 8; ++e) piece[kPieces - 1][e] = (__bf16)rest[e];
 #pragma unroll
-            for (int q = 0; q < kPieces; ++q)
-              O[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values, piece[q], O[dt], 0, 0, 0);
-          }
-        }
+        for (int q = 0; q < kPieces; ++q)
+#pragma unroll
+          for (int dt = 0; dt < 4; ++dt)
+            O[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values[n][dt], piece[q], O[dt], 0, 0, 0);
       }
     };
 
@@ -527,17 +533,28 @@ __global__ __launch_bounds__(64 * kCols *kParts)
     fetch(block0);
     look_up(block0 + 1);
     put(s_rows[0]);
+    // (the queries are waited for here: a load that is pending when the loop begins would be waited for in it, and the
+    // next block's rows with it)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) asm volatile("" ::"v"(Q[k].x), "v"(Q[k].y), "v"(Q[k].z), "v"(Q[k].w));
     __syncthreads();
     for (int b = block0; b < block1; ++b) {
       const int now = S::kBuffers == 1 ? 0 : (b - block0) & 1;
-      if (b + 1 < block1) {
+      const bool more = b + 1 < block1;
+      if (more) {
         fetch(b + 1);
         look_up(b + 2);
-        if (busy) attend(s_rows[now]);
+      }
+      if (busy) {
+#pragma unroll 1
+        for (int u = 0; u < S::kSubs; ++u) {
+          const uint32_t rows = S::kSubs == 1 || u == 0 ? live[0] : live[S::kSubs - 1];
+          if (rows) attend(s_rows[now], (u * kParts + part) * 32, rows);
+        }
+      }
+      if (more) {
         if constexpr (S::kBuffers == 1) __syncthreads();
         put(s_rows[S::kBuffers == 1 ? 0 : now ^ 1]);
-      } else if (busy) {
-        attend(s_rows[now]);
       }
       __syncthreads();
     }
