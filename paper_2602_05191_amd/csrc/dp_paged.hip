@@ -54,6 +54,7 @@ struct PagedArgs {
   int32_t shared_cols;  // columns (sequences x query heads of a KV head) per workgroup over shared rows
   int32_t shared_block; // rows per chunk there
   float scale_log2;
+  float lead;           // 8 / scale_log2: how far a score may lead the reference that is subtracted (shared rows)
 };
 
 // what is subtracted from a score whose running maximum is m
@@ -347,6 +348,9 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
 // All but the last piece are cut, not rounded, and what is left is increased by 2^-23 (three pieces: 2^-26, 2^-34) of the
 // weight: no piece is zero, so that an infinite value does not become NaN (0 x inf).
 // A weight below 2^-126 of the largest counts as zero here (v_exp_f32).
+// What is subtracted from a column's scores is a score that was its largest at some time; it moves when one leads it by 8 in
+// base 2 (weights up to 2^8 lose nothing in fp32 or in pieces).  Moving with every new maximum, some of a wave's 32 columns
+// had one in most tiles: 66 instructions more each time.
 // kCols column tiles x kParts parts of a block's rows = the waves of a workgroup.  A block of 64 or 128 rows goes global ->
 // registers -> LDS while the one before is attended; rows padded to 272 (keys) and 288 (values) bytes.
 template <int kCols, int kParts>
@@ -473,7 +477,7 @@ __global__ __launch_bounds__(64 * kCols *kParts)
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
       top = fmaxf(m, fmaxf(top, xor32(top)));
-      if (top > m) {
+      if (top > m + p.lead) {
         const float alpha = __builtin_amdgcn_exp2f((m - finite_max(top)) * p.scale_log2);
         l *= alpha;
 #pragma unroll
@@ -742,6 +746,7 @@ hipError_t launch_paged_decode(const PagedView &c, const PagedAttention &a, floa
   p.shared_cols = 32 * s.cols;
   p.shared_block = s.shared_block;
   p.scale_log2 = c.sm_scale * kLog2e;
+  p.lead = fminf(8.f / p.scale_log2, 3e38f);
   switch (s.cols) {
     case 1: launch_shared<1, 4>(p, stream); break;
     case 2: launch_shared<2, 4>(p, stream); break;
