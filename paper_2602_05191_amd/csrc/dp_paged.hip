@@ -7,8 +7,9 @@
 //   output  O^T[dims x heads] += V^T P^T, v_mfma_f32_16x16x4_f32 with k = l / 16 standing for row 4 (l / 16) + i: the
 //           weights stay fp32, the values are widened; tile n of eight holds dims 8 x + n.  A tile's 16 rows are summed by
 //           themselves and then added: the fp32 chain is as long as the wave has tiles, not rows.
-// The running maximum is kept and subtracted unscaled, so the largest score has the weight 1 whatever its size; a maximum
-// of -inf is taken as the lowest finite number when it is subtracted; weights keep the range below 2^-126 (exp2f).
+// What is subtracted from a head's scores is a score that was its largest at some time, unscaled (the largest weight is in
+// order whatever the size of the scores); it moves when one leads it by 8 in base 2: weights up to 2^8 lose nothing in fp32.
+// A maximum of -inf is taken as the lowest finite number when it is subtracted; weights keep the range below 2^-126 (exp2f).
 // Tiles begin at multiples of 16 rows, so a tile of pages of 16 tokens or more lies in one page: its place is a scalar and
 // a lane's offsets are the same for every tile.  The numbers of the pages of a wave's next 64 tiles are fetched by its 64
 // lanes at once.  Smaller pages: every row's page by the lane that loads the row's key, a tile ahead of the rows.
@@ -48,13 +49,12 @@ struct PagedArgs {
   AttnOut attn;
   Partials parts;
   int32_t head0;        // this launch serves heads [head0, head0 + 16) of every group
-  int32_t whole;        // own rows: nothing dealt out, a workgroup per segment
-  int32_t direct;       // ... which then writes the output itself
+  int32_t whole;        // own rows: nothing dealt out, a workgroup per segment (which writes the output where none are shared)
   Deal own, shared;     // shared.slots == 0: no shared rows
   int32_t shared_cols;  // columns (sequences x query heads of a KV head) per workgroup over shared rows
   int32_t shared_block; // rows per chunk there
   float scale_log2;
-  float lead;           // 8 / scale_log2: how far a score may lead the reference that is subtracted (shared rows)
+  float lead;           // 8 / scale_log2: how far a score may lead the reference that is subtracted
 };
 
 // what is subtracted from a score whose running maximum is m
@@ -68,17 +68,22 @@ struct SeqRows {
     return first < len ? (len + kChunkRows - 1) / kChunkRows - chunk0() : 0;
   }
 };
+template <bool kShared>
 __device__ __forceinline__ SeqRows seq_rows(const PagedArgs &p, int s) {
   SeqRows r;
   r.len = paged_len(p.c, s);
   int group;
-  r.first = p.shared.slots ? shared_rows(p.c, p.a.shared, s, r.len, group) : p.a.first_rows ? max(0, p.a.first_rows[s]) : 0;
+  if constexpr (kShared)
+    r.first = shared_rows(p.c, p.a.shared, s, r.len, group);
+  else
+    r.first = p.a.first_rows ? max(0, p.a.first_rows[s]) : 0;
   return r;
 }
 // sequences, and the KV heads of each
+template <bool kShared>
 __device__ __forceinline__ auto own_segments(const PagedArgs &p) {
   return [&p](int s) {
-    const SeqRows r = seq_rows(p, s);
+    const SeqRows r = seq_rows<kShared>(p, s);
     return Segments{r.chunks(), p.c.n_kv_heads, r.first, r.len};
   };
 }
@@ -107,11 +112,12 @@ struct TileLoader {
     k_off = kSmallPages ? kq * 16 : r * c.slot_stride + kq * 16;
     v_off = kSmallPages ? r * 16 : 4 * kq * c.slot_stride + r * 16;
   }
-  // (rows behind the last have no entry that may be read)
-  __device__ __forceinline__ int page_of(int row) const { return row < rows.len ? table[row >> c.page_shift] : -1; }
+  // (a row behind the last, whose entry may not be read: the last one's page)
+  __device__ __forceinline__ int page_of(int row) const { return table[min(row, rows.len - 1) >> c.page_shift]; }
   __device__ __forceinline__ void start(int t) {
     t0 = t;
     page = page_of(kSmallPages ? t + (lane_id() & 15) : t + lane_id() * kStep);
+    asm volatile("" ::"v"(page));  // waited for here: in front of a tile's loads all loads would be waited for
   }
   __device__ __forceinline__ bool there(int p) const { return (uint32_t)p < (uint32_t)c.n_pages; }
   __device__ __forceinline__ int64_t place(int p, int row) const {
@@ -133,6 +139,7 @@ struct TileLoader {
       for (int i = 0; i < 4; ++i) d.v[i] = load_stream16(vr + (v_off + i * c.slot_stride));
     } else {
       const int r = lane_id() & 15, kq = lane_id() >> 4;
+      const int next = page_of(t + kStep + r);  // (in front of the rows: it is waited for before they are)
       const bool ok = there(page);
       live &= (uint32_t)__ballot(ok);
       const int64_t at = place(ok ? page : 0, t + r);
@@ -146,7 +153,7 @@ struct TileLoader {
                                          (uint32_t)__shfl((int)at, row, 64));
         d.v[i] = load_stream16(v + of_row + v_off);
       }
-      page = page_of(t + kStep + r);
+      page = next;
     }
     d.live = live;
   }
@@ -168,10 +175,11 @@ __device__ __forceinline__ void store_head(const PagedArgs &p, int64_t head, int
   if (p.attn.lse && d == 0) p.attn.lse[head] = any ? (M + log2f(L)) * kLn2 : -INFINITY;
 }
 
-template <bool kSmallPages>
+template <bool kSmallPages, bool kShared>
 __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_kernel(PagedArgs p) {
   __shared__ float s_m[kPagedWaves][kPagedHeads], s_l[kPagedWaves][kPagedHeads];
   __shared__ __align__(16) float s_acc[kPagedWaves][kPagedHeads][kHeadDim + 4];
+  __shared__ float s_prior[kPagedHeads];
   const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
   const int r = lane & 15, kq = lane >> 4;
   const int n_kv = p.c.n_kv_heads, group = p.c.group, n_live = min(kPagedHeads, group - p.head0);
@@ -179,11 +187,11 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
   if (p.whole) {
     at.i = blockIdx.x / n_kv;
     at.sub = blockIdx.x % n_kv;
-    at.item = own_segments(p)(at.i);
+    at.item = own_segments<kShared>(p)(at.i);
     at.first = at.c = 0;
     at.c_end = at.item.chunks;
     at.share = 1;
-  } else if (!deal_start(p.own, p.c.n_seqs, own_segments(p), at)) {
+  } else if (!deal_start(p.own, p.c.n_seqs, own_segments<kShared>(p), at)) {
     return;
   }
 
@@ -206,7 +214,7 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
     f32x4 acc[8];
 #pragma unroll
     for (int n = 0; n < 8; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;  // head r: the largest score so far (unscaled), the weights of this lane's rows
+    float m = -INFINITY, l = 0.f;  // head r: the score that is subtracted, the weights of this lane's rows
 
     auto attend = [&](PagedTile &d) {
       const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -228,7 +236,7 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
       top = fmaxf(top, xor16(top));
       top = fmaxf(top, xor32(top));
       top = fmaxf(m, top);
-      if (__ballot(top > m)) {
+      if (__ballot(top > m + p.lead)) {
         const float alpha = exp2f((m - finite_max(top)) * p.scale_log2);
         l *= alpha;
 #pragma unroll
@@ -293,24 +301,16 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
         dst[1] = make_float4(acc[4][i], acc[5][i], acc[6][i], acc[7][i]);
       }
     }
-    // (what was known before is read before any of it may be overwritten)
-    constexpr int kMost = kPagedHeads / (kPagedThreads / kHeadDim);
-    const int d = tid % kHeadDim, j0 = tid / kHeadDim;
-    float prior_o[kMost], prior_lse[kMost];
-    if (p.direct && p.a.prior_lse) {
-#pragma unroll
-      for (int u = 0; u < kMost; ++u) {
-        const int64_t head = head_first + min(j0 + u * (kPagedThreads / kHeadDim), n_live - 1);
-        prior_o[u] = p.a.prior_out[head * kHeadDim + d];
-        prior_lse[u] = p.a.prior_lse[head];
-      }
+    const bool direct = !kShared && p.whole;
+    if (!kShared) {  // (read before any of it may be overwritten)
+      if (tid < n_live) s_prior[tid] = direct && p.a.prior_lse ? p.a.prior_lse[head_first + tid] : -INFINITY;
     }
     __syncthreads();
     // thread t: dim t % 128 of heads t / 128, t / 128 + 2, ...
-#pragma unroll
-    for (int u = 0; u < kMost; ++u) {
-      const int j = j0 + u * (kPagedThreads / kHeadDim);
-      if (j >= n_live) break;
+    const int d = tid % kHeadDim;
+#pragma unroll 2
+    for (int j = tid / kHeadDim; j < n_live; j += kPagedThreads / kHeadDim) {
+      const float prior_o = direct && p.a.prior_lse ? p.a.prior_out[(head_first + j) * kHeadDim + d] : 0.f;
       Merged x{-INFINITY, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < kPagedWaves; ++w) x.m = fmaxf(x.m, s_m[w][j]);
@@ -320,8 +320,8 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
         x.l += s_l[w][j] * wg;
         x.o += s_acc[w][j][d] * wg;
       }
-      if (p.direct) {
-        store_head(p, head_first + j, d, p.a.prior_lse ? prior_lse[u] : -INFINITY, p.a.prior_lse ? prior_o[u] : 0.f, x);
+      if (direct) {
+        store_head(p, head_first + j, d, s_prior[j], prior_o, x);
         continue;
       }
       const int64_t slot = (head_first + j) * p.parts.all + split;
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
     }
     if (seg_end >= at.c_end) break;
     __syncthreads();  // LDS is reused by the next piece
-    deal_next(own_segments(p), at);
+    deal_next(own_segments<kShared>(p), at);
   }
 }
 
@@ -419,7 +419,7 @@ __global__ __launch_bounds__(64 * kCols *kParts)
     int pages[S::kLoads], live_page[S::kSubs];
     uint4 kr[S::kLoads], vr[S::kLoads];
     uint32_t live[S::kSubs], live_next[S::kSubs], here = 0;  // here: bit i for the row of load i
-    auto page_of = [&](int row) { return row < grp.rows ? table[row >> c.page_shift] : -1; };
+    auto page_of = [&](int row) { return table[min(row, grp.rows - 1) >> c.page_shift]; };
     auto look_up = [&](int block) {
 #pragma unroll
       for (int i = 0; i < S::kLoads; ++i) pages[i] = page_of(block * S::kRows + i * kRowsPerLoad + (tid >> 4));
@@ -431,7 +431,7 @@ __global__ __launch_bounds__(64 * kCols *kParts)
 #pragma unroll
       for (int i = 0; i < S::kLoads; ++i) {
         const int row = block * S::kRows + i * kRowsPerLoad + (tid >> 4);
-        const bool there = (uint32_t)pages[i] < (uint32_t)c.n_pages;
+        const bool there = (uint32_t)pages[i] < (uint32_t)c.n_pages && row < grp.rows;
         const int64_t place = (there ? pages[i] : 0) * c.page_stride + (row & ((1 << c.page_shift) - 1)) * (int64_t)c.slot_stride;
         kr[i] = load_stream16(k_head + place);
         vr[i] = load_stream16(v_head + place);
@@ -439,7 +439,8 @@ __global__ __launch_bounds__(64 * kCols *kParts)
       }
 #pragma unroll
       for (int u = 0; u < S::kSubs; ++u)
-        live_next[u] = (uint32_t)__ballot((uint32_t)live_page[u] < (uint32_t)c.n_pages);
+        live_next[u] = (uint32_t)__ballot((uint32_t)live_page[u] < (uint32_t)c.n_pages &&
+                                          block * S::kRows + (u * kParts + part) * 32 + (lane & 31) < grp.rows);
     };
     auto put = [&](char *buffer) {  // (values of rows that are not there: zero)
 #pragma unroll
@@ -609,16 +610,16 @@ __global__ __launch_bounds__(64 * kCols *kParts)
 
 // One workgroup per head; its groups of 128 threads (one dimension each) take the pieces in turn, so that the partials of
 // a head are fetched in a round or two of loads, and meet in LDS.
-template <int kGroups>
+template <int kGroups, bool kShared>
 __global__ __launch_bounds__(kGroups * kHeadDim) void paged_merge_kernel(PagedArgs p) {
   __shared__ float s_m[kGroups], s_l[kGroups], s_o[kGroups][kHeadDim];
   const int head = blockIdx.x, t = threadIdx.x % kHeadDim, grp = threadIdx.x / kHeadDim;
   const int seq = head / p.c.n_q_heads, kv = head % p.c.n_q_heads / p.c.group;
-  const SeqRows rows = seq_rows(p, seq);
+  const SeqRows rows = seq_rows<kShared>(p, seq);
   const int chunks = rows.chunks();
-  const int n_own = p.whole ? 1 : chunks ? deal_pieces(p.own, p.c.n_seqs, own_segments(p), seq, kv, chunks) : 0;
+  const int n_own = p.whole ? 1 : chunks ? deal_pieces(p.own, p.c.n_seqs, own_segments<kShared>(p), seq, kv, chunks) : 0;
   int n_active = n_own;
-  if (p.shared.slots && rows.first > 0) {
+  if (kShared && rows.first > 0) {
     int g;
     shared_rows(p.c, p.a.shared, seq, rows.len, g);
     const Segments s = shared_segments(p)(g);
@@ -719,6 +720,23 @@ void launch_shared(const PagedArgs &p, hipStream_t stream) {
     hipLaunchKernelGGL((shared_kernel<kCols, kParts, 3>), dim3(p.shared.grid), dim3(S::kThreads), 0, stream, p);
 }
 
+template <bool kShared>
+void launch_own(PagedArgs &p, hipStream_t stream) {
+  const int nh = p.c.n_seqs * p.c.n_q_heads;
+  const dim3 grid(p.whole ? p.c.n_seqs * p.c.n_kv_heads : p.own.grid), block(kPagedThreads);
+  for (p.head0 = 0; p.head0 < p.c.group; p.head0 += kPagedHeads) {  // one pass over the rows for up to 16 heads of a group
+    if (p.c.page_shift < 4)
+      hipLaunchKernelGGL((paged_kernel<true, kShared>), grid, block, 0, stream, p);
+    else
+      hipLaunchKernelGGL((paged_kernel<false, kShared>), grid, block, 0, stream, p);
+  }
+  if (p.whole && !kShared) return;
+  if (nh >= 512 || p.c.max_seq_len <= 32 * kChunkRows)
+    hipLaunchKernelGGL((paged_merge_kernel<1, kShared>), dim3(nh), dim3(kHeadDim), 0, stream, p);
+  else
+    hipLaunchKernelGGL((paged_merge_kernel<8, kShared>), dim3(nh), dim3(8 * kHeadDim), 0, stream, p);
+}
+
 }  // namespace
 
 size_t paged_partials(const PagedView &c, const SharedView &shared) {
@@ -740,7 +758,6 @@ hipError_t launch_paged_decode(const PagedView &c, const PagedAttention &a, floa
   p.parts.acc = partials;
   p.parts.ml = reinterpret_cast<float2 *>(partials + (size_t)nh * p.parts.all * kHeadDim);
   p.whole = s.whole;
-  p.direct = s.whole && !s.shared.slots;
   p.own = s.own;
   p.shared = s.shared;
   p.shared_cols = 32 * s.cols;
@@ -753,18 +770,10 @@ hipError_t launch_paged_decode(const PagedView &c, const PagedAttention &a, floa
     case 4: launch_shared<4, 2>(p, stream); break;
     case 8: launch_shared<8, 1>(p, stream); break;
   }
-  const dim3 grid(s.whole ? c.n_seqs * c.n_kv_heads : s.own.grid), block(kPagedThreads);
-  for (p.head0 = 0; p.head0 < c.group; p.head0 += kPagedHeads) {  // one pass over the rows for up to 16 heads of a group
-    if (c.page_shift < 4)
-      hipLaunchKernelGGL(paged_kernel<true>, grid, block, 0, stream, p);
-    else
-      hipLaunchKernelGGL(paged_kernel<false>, grid, block, 0, stream, p);
-  }
-  if (p.direct) return hipGetLastError();
-  if (nh >= 512 || c.max_seq_len <= 32 * kChunkRows)
-    hipLaunchKernelGGL(paged_merge_kernel<1>, dim3(nh), dim3(kHeadDim), 0, stream, p);
+  if (s.shared.slots)
+    launch_own<true>(p, stream);
   else
-    hipLaunchKernelGGL(paged_merge_kernel<8>, dim3(nh), dim3(8 * kHeadDim), 0, stream, p);
+    launch_own<false>(p, stream);
   return hipGetLastError();
 }
 
