@@ -33,61 +33,6 @@ constexpr int kPagedThreads = 256;
 constexpr int kPagedWaves = kPagedThreads / 64;
 constexpr int kPagedHeads = 16;  // query heads per pass: the columns of one MFMA tile
 constexpr int kPagedTile = 16;   // rows per wave and step
-constexpr int kDealtItems = 64 * 64;  // most sequences, or groups, that the lookup of a share can hold
-
-// Partial results of a head: per slot the accumulator of its 128 dimensions, (maximum in base 2, sum).  The slots of its
-// own rows come first, then those of the rows that it shares.
-struct Partials {
-  float *acc;
-  float2 *ml;
-  int32_t own, all;  // slots per head
-};
-
-struct PagedArgs {
-  PagedView c;
-  PagedAttention a;
-  AttnOut attn;
-  Partials parts;
-  int32_t head0;        // this launch serves heads [head0, head0 + 16) of every group
-  int32_t whole;        // own rows: nothing dealt out, a workgroup per segment (which writes the output where none are shared)
-  Deal own, shared;     // shared.slots == 0: no shared rows
-  int32_t shared_cols;  // columns (sequences x query heads of a KV head) per workgroup over shared rows
-  int32_t shared_block; // rows per chunk there
-  float scale_log2;
-  float lead;           // 8 / scale_log2: how far a score may lead the reference that is subtracted
-};
-
-// what is subtracted from a score whose running maximum is m
-__device__ __forceinline__ float finite_max(float m) { return fmaxf(m, -3.402823466e38f); }
-
-// Rows [first, len) of a sequence; its chunks are [first / 64, ceil(len / 64)).
-struct SeqRows {
-  int first, len;
-  __device__ __forceinline__ int chunk0() const { return first / kChunkRows; }
-  __device__ __forceinline__ int chunks() const {
-    return first < len ? (len + kChunkRows - 1) / kChunkRows - chunk0() : 0;
-  }
-};
-template <bool kShared>
-__device__ __forceinline__ SeqRows seq_rows(const PagedArgs &p, int s) {
-  SeqRows r;
-  r.len = paged_len(p.c, s);
-  int group;
-  if constexpr (kShared)
-    r.first = shared_rows(p.c, p.a.shared, s, r.len, group);
-  else
-    r.first = p.a.first_rows ? max(0, p.a.first_rows[s]) : 0;
-  return r;
-}
-// sequences, and the KV heads of each
-template <bool kShared>
-__device__ __forceinline__ auto own_segments(const PagedArgs &p) {
-  return [&p](int s) {
-    const SeqRows r = seq_rows<kShared>(p, s);
-    return Segments{r.chunks(), p.c.n_kv_heads, r.first, r.len};
-  };
-}
-
 // one wave's 16 rows as the two contractions want them, and which of them count
 struct PagedTile {
   uint4 k[4], v[4];
@@ -334,280 +279,6 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
   }
 }
 
-// ---- rows that a group shares ----
-// The columns are the queries of all sequences of the group, G per sequence: with tens of columns and more the products
-// are large enough for the matrix cores' bf16 rate, and the rows are read once for all of them.
-//   scores  S^T[32 rows x 32 columns] = K Q^T, v_mfma_f32_32x32x16_bf16, the keys from LDS, the queries in registers: a
-//           lane holds 16 scores of column lane % 32, rows 8 (i / 4) + 4 (lane / 32) + i % 4;
-//   output  O^T[dims x columns] += V^T P^T, the same instruction: weights i = 8 n .. 8 n + 7 of a lane are the k = 8
-//           (lane / 32) .. + 7 of the n-th 16 rows if the values come in that order of rows, and they do: ds_read_tr16_b64
-//           hands a lane one dimension of four consecutive rows, two of them the eight rows 16 n + 4 (lane / 32) + {0 .. 3,
-//           8 .. 11}.  Nothing moves between lanes but the two halves' maxima.
-// Weights go into the product in bf16 pieces that add up: two (16 bits) for a bf16 output, three (all 24) for fp32; their
-// sum is taken from the fp32 weights.  (One piece rounds a weight by up to 2^-9, as much as the output itself is rounded.)
-// All but the last piece are cut, not rounded, and what is left is increased by 2^-23 (three pieces: 2^-26, 2^-34) of the
-// weight: no piece is zero, so that an infinite value does not become NaN (0 x inf).
-// A weight below 2^-126 of the largest counts as zero here (v_exp_f32).
-// What is subtracted from a column's scores is a score that was its largest at some time; it moves when one leads it by 8 in
-// base 2 (weights up to 2^8 lose nothing in fp32 or in pieces).  Moving with every new maximum, some of a wave's 32 columns
-// had one in most tiles: 66 instructions more each time.
-// kCols column tiles x kParts parts of a block's rows = the waves of a workgroup.  A block of 64 or 128 rows goes global ->
-// registers -> LDS while the one before is attended; rows padded to 272 (keys) and 288 (values) bytes.
-template <int kCols, int kParts>
-struct SharedShape {
-  static constexpr int kWaves = kCols * kParts, kThreads = 64 * kWaves;
-  static constexpr int kRows = kParts * 32 < 64 ? 64 : kParts * 32;
-  static constexpr int kSubs = kRows / (32 * kParts);  // 32-row tiles of a wave in a block
-  static constexpr int kLoads = kRows * 16 / kThreads;  // 16-byte loads of a thread per block, of keys and of values
-  static constexpr int kBuffers = kWaves == 4 ? 1 : 2;
-  static constexpr int kKPitch = 272, kVPitch = 288;
-  static constexpr int kBuffer = kRows * (kKPitch + kVPitch);
-  static constexpr int kResident = kWaves == 4 ? 512 : 256;  // two waves per SIMD
-};
-
-// groups; their KV heads, and of each the column tiles of a workgroup
-__device__ __forceinline__ auto shared_segments(const PagedArgs &p) {
-  return [&p](int g) {
-    const SharedGroup s = shared_group(p.c, p.a.shared, g);
-    const int tiles = ((s.end - s.begin) * p.c.group + p.shared_cols - 1) / p.shared_cols;
-    return Segments{(s.rows + p.shared_block - 1) / p.shared_block, p.c.n_kv_heads * tiles, s.begin, s.reader};
-  };
-}
-
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4 *LdsTile;
-
-template <int kCols, int kParts, int kPieces>
-__global__ __launch_bounds__(64 * kCols *kParts)
-    __attribute__((amdgpu_waves_per_eu(2, 2))) void shared_kernel(PagedArgs p) {
-  using S = SharedShape<kCols, kParts>;
-  __shared__ __align__(16) char s_rows[S::kBuffers][S::kBuffer];
-  const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
-  const int col_tile = wave % kCols, part = wave / kCols, half = lane >> 5;
-  const PagedView &c = p.c;
-  Dealt at;
-  if (!deal_start(p.shared, p.a.shared.n_groups, shared_segments(p), at)) return;
-
-  while (true) {
-    const SharedGroup grp = shared_group(c, p.a.shared, at.i);
-    const int tiles = at.item.subs / c.n_kv_heads, kv = at.sub / tiles, col0 = at.sub % tiles * p.shared_cols + 32 * col_tile;
-    const int n_cols = (grp.end - grp.begin) * c.group;
-    const int split = blockIdx.x - at.first / at.share, seg_end = at.first + at.item.chunks;
-    const int block0 = at.c - at.first, block1 = min(at.c_end, seg_end) - at.first;
-    const int32_t *table = c.table + (int64_t)grp.reader * c.table_stride;
-    const bool busy = col0 < n_cols;
-
-    // the lane's column: a query head of one of the sequences
-    const int col = min(col0 + (lane & 31), n_cols - 1), col_seq = grp.begin + col / c.group;
-    const int64_t head = (int64_t)col_seq * c.n_q_heads + kv * c.group + col % c.group;
-    const bool mine = col0 + (lane & 31) < n_cols && paged_len(c, col_seq) >= grp.rows;
-    uint4 Q[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      Q[k] = *reinterpret_cast<const uint4 *>(static_cast<const char *>(p.a.q) + head * kRowBytes + k * 32 + half * 16);
-    f32x16 O[4];
-#pragma unroll
-    for (int n = 0; n < 4; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) O[n][i] = 0.f;
-    float m = -INFINITY, l = 0.f;
-
-    // ---- a block's rows: 16 lanes per row, kLoads rows per thread; pages looked up a block ahead ----
-    constexpr int kRowsPerLoad = S::kThreads / 16;
-    const char *k_head = c.k_pages + kv * c.head_stride + (tid & 15) * 16, *v_head = c.v_pages + kv * c.head_stride + (tid & 15) * 16;
-    int pages[S::kLoads], live_page[S::kSubs];
-    uint4 kr[S::kLoads], vr[S::kLoads];
-    uint32_t live[S::kSubs], live_next[S::kSubs], here = 0;  // here: bit i for the row of load i
-    auto page_of = [&](int row) { return table[min(row, grp.rows - 1) >> c.page_shift]; };
-    auto look_up = [&](int block) {
-#pragma unroll
-      for (int i = 0; i < S::kLoads; ++i) pages[i] = page_of(block * S::kRows + i * kRowsPerLoad + (tid >> 4));
-#pragma unroll
-      for (int u = 0; u < S::kSubs; ++u) live_page[u] = page_of(block * S::kRows + (u * kParts + part) * 32 + (lane & 31));
-    };
-    auto fetch = [&](int block) {
-      here = 0;
-#pragma unroll
-      for (int i = 0; i < S::kLoads; ++i) {
-        const int row = block * S::kRows + i * kRowsPerLoad + (tid >> 4);
-        const bool there = (uint32_t)pages[i] < (uint32_t)c.n_pages && row < grp.rows;
-        const int64_t place = (there ? pages[i] : 0) * c.page_stride + (row & ((1 << c.page_shift) - 1)) * (int64_t)c.slot_stride;
-        kr[i] = load_stream16(k_head + place);
-        vr[i] = load_stream16(v_head + place);
-        here |= (uint32_t)there << i;
-      }
-#pragma unroll
-      for (int u = 0; u < S::kSubs; ++u)
-        live_next[u] = (uint32_t)__ballot((uint32_t)live_page[u] < (uint32_t)c.n_pages &&
-                                          block * S::kRows + (u * kParts + part) * 32 + (lane & 31) < grp.rows);
-    };
-    auto put = [&](char *buffer) {  // (values of rows that are not there: zero)
-#pragma unroll
-      for (int i = 0; i < S::kLoads; ++i) {
-        const int row = i * kRowsPerLoad + (tid >> 4);
-        *reinterpret_cast<uint4 *>(buffer + row * S::kKPitch + (tid & 15) * 16) = kr[i];
-        *reinterpret_cast<uint4 *>(buffer + S::kRows * S::kKPitch + row * S::kVPitch + (tid & 15) * 16) =
-            here >> i & 1 ? vr[i] : make_uint4(0, 0, 0, 0);
-      }
-#pragma unroll
-      for (int u = 0; u < S::kSubs; ++u) live[u] = live_next[u];
-    };
-
-    // one 32-row tile of a block
-    auto attend = [&](const char *buffer, int row0, uint32_t live) {
-      const char *k = buffer + (row0 + (lane & 31)) * S::kKPitch + half * 16;
-      uint4 key[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) key[j] = *reinterpret_cast<const uint4 *>(k + 32 * j);
-      f32x16 x;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, key[j]), __builtin_bit_cast(bf16x8, Q[j]), x,
-                                                    0, 0, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);  // (all reads, then the products)
-      __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
-      if (live != 0xffffffffu) {
-        const uint32_t on = live >> (4 * half);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = on & 1u << (8 * (i / 4) + i % 4) ? x[i] : -INFINITY;
-      }
-      float top = x[0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-      top = fmaxf(m, fmaxf(top, xor32(top)));
-      if (top > m + p.lead) {
-        const float alpha = __builtin_amdgcn_exp2f((m - finite_max(top)) * p.scale_log2);
-        l *= alpha;
-#pragma unroll
-        for (int n = 0; n < 4; ++n) O[n] *= alpha;
-        m = top;
-      }
-      const float sub = finite_max(m);
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        x[i] = __builtin_amdgcn_exp2f((x[i] - sub) * p.scale_log2);
-        sum += x[i];
-      }
-      l += sum;
-      // the value rows 4 half + (lane % 16) / 4 of a quad, dims 16 (lane / 16 % 2) + 4 (lane % 4)
-      const char *v = buffer + S::kRows * S::kKPitch + (row0 + 4 * half + (lane & 15) / 4) * S::kVPitch +
-                      (lane >> 4 & 1) * 32 + (lane & 3) * 8;
-      bf16x8 values[2][4];
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt) {
-          const char *at = v + n * 16 * S::kVPitch + dt * 64;
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsTile)(at));
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsTile)(at + 8 * S::kVPitch));
-          values[n][dt] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        }
-      __builtin_amdgcn_sched_group_barrier(0x100, 16, 0);  // (the reads are on their way during the exponentials)
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        float rest[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) rest[e] = x[8 * n + e];
-        bf16x8 piece[kPieces];
-#pragma unroll
-        for (int q = 0; q + 1 < kPieces; ++q)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float cut = __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
-            piece[q][e] = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(rest[e]) >> 16));
-            if (kPieces == 2)
-              rest[e] = fmaf(rest[e], 1.f + 0x1p-23f, -cut);
-            else
-              rest[e] = fmaf(x[8 * n + e], q == 0 ? 0x1p-26f : 0x1p-34f, rest[e] - cut);
-          }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) piece[kPieces - 1][e] = (__bf16)rest[e];
-#pragma unroll
-        for (int q = 0; q < kPieces; ++q)
-#pragma unroll
-          for (int dt = 0; dt < 4; ++dt)
-            O[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values[n][dt], piece[q], O[dt], 0, 0, 0);
-      }
-    };
-
-    look_up(block0);
-    fetch(block0);
-    look_up(block0 + 1);
-    put(s_rows[0]);
-    // (the queries are waited for here: a load that is pending when the loop begins would be waited for in it, and the
-    // next block's rows with it)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) asm volatile("" ::"v"(Q[k].x), "v"(Q[k].y), "v"(Q[k].z), "v"(Q[k].w));
-    __syncthreads();
-    for (int b = block0; b < block1; ++b) {
-      const int now = S::kBuffers == 1 ? 0 : (b - block0) & 1;
-      const bool more = b + 1 < block1;
-      if (more) {
-        fetch(b + 1);
-        look_up(b + 2);
-      }
-      if (busy) {
-#pragma unroll 1
-        for (int u = 0; u < S::kSubs; ++u) {
-          const uint32_t rows = S::kSubs == 1 || u == 0 ? live[0] : live[S::kSubs - 1];
-          if (rows) attend(s_rows[now], (u * kParts + part) * 32, rows);
-        }
-      }
-      if (more) {
-        if constexpr (S::kBuffers == 1) __syncthreads();
-        put(s_rows[S::kBuffers == 1 ? 0 : now ^ 1]);
-      }
-      __syncthreads();
-    }
-    l += xor32(l);
-
-    // the parts of the rows meet in LDS, in pairs
-    m *= p.scale_log2;
-    float *meet = reinterpret_cast<float *>(&s_rows[0][0]);
-    static_assert(kParts == 1 || (kCols * kParts / 2) * 66 * 64 * 4 <= S::kBuffers * S::kBuffer, "the halves fit the buffers");
-#pragma unroll
-    for (int step = kParts / 2; step > 0; step /= 2) {
-      float *slot = meet + (part % step * kCols + col_tile) * 66 * 64 + lane;
-      if (part >= step && part < 2 * step) {
-        slot[64 * 64] = m;
-        slot[65 * 64] = l;
-#pragma unroll
-        for (int n = 0; n < 4; ++n)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) slot[(16 * n + i) * 64] = O[n][i];
-      }
-      __syncthreads();
-      if (part < step) {
-        const float mo = slot[64 * 64], top = fmaxf(m, mo), sub = finite_max(top);
-        const float w = __builtin_amdgcn_exp2f(m - sub), wo = __builtin_amdgcn_exp2f(mo - sub);
-        l = fmaf(l, w, slot[65 * 64] * wo);
-#pragma unroll
-        for (int n = 0; n < 4; ++n)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) O[n][i] = fmaf(O[n][i], w, slot[(16 * n + i) * 64] * wo);
-        m = top;
-      }
-      __syncthreads();
-    }
-
-    if (busy && mine && part == 0) {
-      const int64_t slot = head * p.parts.all + p.parts.own + split;
-      if (half == 0) p.parts.ml[slot] = make_float2(m, l);
-      float4 *dst = reinterpret_cast<float4 *>(p.parts.acc + slot * kHeadDim + 4 * half);
-#pragma unroll
-      for (int n = 0; n < 4; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dst[8 * n + 2 * i] = make_float4(O[n][4 * i], O[n][4 * i + 1], O[n][4 * i + 2], O[n][4 * i + 3]);
-    }
-    if (seg_end >= at.c_end) break;
-    deal_next(shared_segments(p), at);
-  }
-}
-
 // One workgroup per head; its groups of 128 threads (one dimension each) take the pieces in turn, so that the partials of
 // a head are fetched in a round or two of loads, and meet in LDS.
 template <int kGroups, bool kShared>
@@ -684,9 +355,8 @@ __global__ __launch_bounds__(kGroups * kHeadDim) void paged_merge_kernel(PagedAr
 
 // How a call is split; by sizes that the host knows.
 struct Split {
-  int whole, cols, parts;  // own rows; shared rows: the shape of a workgroup
+  int whole, cols;  // own rows; shared rows: columns of a workgroup
   Deal own, shared;
-  int shared_block;
 };
 int at_most(long n, long most) { return (int)(n < most ? n : most); }
 int at_least(long n, long least) { return (int)(n > least ? n : least); }
@@ -701,23 +371,12 @@ Split split_of(const PagedView &c, const SharedView &shared) {
   s.own.slots = s.whole ? 1 : at_least(at_most(max_chunks, at_most(at_least(16384 / nh, 8), kMaxSplits)), 1);
   if (shared.n_groups == 0 || shared.max_shared_len == 0 || shared.n_groups > kDealtItems) return s;
   const long cols = (long)(shared.max_group_seqs < c.n_seqs ? shared.max_group_seqs : c.n_seqs) * c.group;
-  s.cols = cols <= 32 ? 1 : cols <= 64 ? 2 : cols <= 128 ? 4 : 8;
-  s.parts = s.cols == 1 ? 4 : 8 / s.cols;
-  s.shared_block = s.parts * 32 < 64 ? 64 : s.parts * 32;
-  s.shared.grid = s.cols == 1 ? 512 : 256;
-  // a segment has at most ceil(grid / KV heads) + 1 pieces
-  const int max_blocks = (shared.max_shared_len + s.shared_block - 1) / s.shared_block;
+  s.cols = cols <= 128 ? 128 : 256;
+  // one workgroup per CU; a segment has at most ceil(grid / KV heads) + 1 pieces
+  s.shared.grid = 256;
+  const int max_blocks = (shared.max_shared_len + kSharedBlock - 1) / kSharedBlock;
   s.shared.slots = at_most(at_most(max_blocks, s.shared.grid / c.n_kv_heads + 2), at_least(131072 / nh, 8));
   return s;
-}
-
-template <int kCols, int kParts>
-void launch_shared(const PagedArgs &p, hipStream_t stream) {
-  using S = SharedShape<kCols, kParts>;
-  if (p.attn.out_is_bf16)
-    hipLaunchKernelGGL((shared_kernel<kCols, kParts, 2>), dim3(p.shared.grid), dim3(S::kThreads), 0, stream, p);
-  else
-    hipLaunchKernelGGL((shared_kernel<kCols, kParts, 3>), dim3(p.shared.grid), dim3(S::kThreads), 0, stream, p);
 }
 
 template <bool kShared>
@@ -748,7 +407,6 @@ size_t paged_partials(const PagedView &c, const SharedView &shared) {
 hipError_t launch_paged_decode(const PagedView &c, const PagedAttention &a, float *partials, const AttnOut &attn,
                                hipStream_t stream) {
   const Split s = split_of(c, a.shared);
-  const int nh = c.n_seqs * c.n_q_heads;
   PagedArgs p{};
   p.c = c;
   p.a = a;
@@ -756,24 +414,19 @@ hipError_t launch_paged_decode(const PagedView &c, const PagedAttention &a, floa
   p.parts.own = s.own.slots;
   p.parts.all = s.own.slots + s.shared.slots;
   p.parts.acc = partials;
-  p.parts.ml = reinterpret_cast<float2 *>(partials + (size_t)nh * p.parts.all * kHeadDim);
+  p.parts.ml = reinterpret_cast<float2 *>(partials + (size_t)c.n_seqs * c.n_q_heads * p.parts.all * kHeadDim);
   p.whole = s.whole;
   p.own = s.own;
   p.shared = s.shared;
-  p.shared_cols = 32 * s.cols;
-  p.shared_block = s.shared_block;
+  p.shared_cols = s.cols;
   p.scale_log2 = c.sm_scale * kLog2e;
   p.lead = fminf(8.f / p.scale_log2, 3e38f);
-  switch (s.cols) {
-    case 1: launch_shared<1, 4>(p, stream); break;
-    case 2: launch_shared<2, 4>(p, stream); break;
-    case 4: launch_shared<4, 2>(p, stream); break;
-    case 8: launch_shared<8, 1>(p, stream); break;
-  }
-  if (s.shared.slots)
+  if (s.shared.slots) {
+    launch_shared_rows(p, stream);
     launch_own<true>(p, stream);
-  else
+  } else {
     launch_own<false>(p, stream);
+  }
   return hipGetLastError();
 }
 

@@ -142,4 +142,72 @@ __device__ __forceinline__ int deal_pieces(const Deal &deal, int n, At at, int i
   return (first + chunks - 1) / share - first / share + 1;
 }
 
+// ---- a call, as its kernels see it ----
+constexpr int kSharedBlock = 64;       // shared rows per chunk
+constexpr int kDealtItems = 64 * 64;  // most sequences, or groups, that the lookup of a share can hold
+
+// Partial results of a head: per slot the accumulator of its 128 dimensions, (maximum in base 2, sum).  The slots of its
+// own rows come first, then those of the rows that it shares.
+struct Partials {
+  float *acc;
+  float2 *ml;
+  int32_t own, all;  // slots per head
+};
+
+struct PagedArgs {
+  PagedView c;
+  PagedAttention a;
+  AttnOut attn;
+  Partials parts;
+  int32_t head0;        // this launch serves heads [head0, head0 + 16) of every group
+  int32_t whole;        // own rows: nothing dealt out, a workgroup per segment (which writes the output where none are shared)
+  Deal own, shared;     // shared.slots == 0: no shared rows
+  int32_t shared_cols;  // columns (sequences x query heads of a KV head) per workgroup over shared rows
+  float scale_log2;
+  float lead;           // 8 / scale_log2: how far a score may lead the reference that is subtracted
+};
+
+// what is subtracted from a score whose running maximum is m
+__device__ __forceinline__ float finite_max(float m) { return fmaxf(m, -3.402823466e38f); }
+
+// Rows [first, len) of a sequence; its chunks are [first / 64, ceil(len / 64)).
+struct SeqRows {
+  int first, len;
+  __device__ __forceinline__ int chunk0() const { return first / kChunkRows; }
+  __device__ __forceinline__ int chunks() const {
+    return first < len ? (len + kChunkRows - 1) / kChunkRows - chunk0() : 0;
+  }
+};
+template <bool kShared>
+__device__ __forceinline__ SeqRows seq_rows(const PagedArgs &p, int s) {
+  SeqRows r;
+  r.len = paged_len(p.c, s);
+  int group;
+  if constexpr (kShared)
+    r.first = shared_rows(p.c, p.a.shared, s, r.len, group);
+  else
+    r.first = p.a.first_rows ? max(0, p.a.first_rows[s]) : 0;
+  return r;
+}
+// sequences, and the KV heads of each
+template <bool kShared>
+__device__ __forceinline__ auto own_segments(const PagedArgs &p) {
+  return [&p](int s) {
+    const SeqRows r = seq_rows<kShared>(p, s);
+    return Segments{r.chunks(), p.c.n_kv_heads, r.first, r.len};
+  };
+}
+
+// groups; their KV heads, and of each the column tiles of a workgroup
+__device__ __forceinline__ auto shared_segments(const PagedArgs &p) {
+  return [&p](int g) {
+    const SharedGroup s = shared_group(p.c, p.a.shared, g);
+    const int tiles = ((s.end - s.begin) * p.c.group + p.shared_cols - 1) / p.shared_cols;
+    return Segments{(s.rows + kSharedBlock - 1) / kSharedBlock, p.c.n_kv_heads * tiles, s.begin, s.reader};
+  };
+}
+
+// The attention of shared rows: one launch that leaves partial results (dp_shared.hip).  Columns per workgroup: 256 or 128.
+void launch_shared_rows(const PagedArgs &p, hipStream_t stream);
+
 }  // namespace dp
