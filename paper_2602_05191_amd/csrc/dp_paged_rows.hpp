@@ -80,7 +80,7 @@ struct Dealt {
 // By every wave for itself: a lane adds up `per` consecutive items, then the lane that holds chunk c has its items spread
 // over the lanes.  n <= 64 * 64.  false: no chunk is left.
 template <class At>
-__device__ __forceinline__ bool deal_start(const Deal &deal, int n, At at, Dealt &d) {
+__device__ __forceinline__ bool deal_start(const Deal &deal, int block, int n, At at, Dealt &d) {
   const int lane = lane_id(), per = (n + 63) / 64;
   Segments item{0, 0, 0, 0};
   auto look = [&](int i, bool valid) {
@@ -96,7 +96,7 @@ __device__ __forceinline__ bool deal_start(const Deal &deal, int n, At at, Dealt
   int upto = wave_incl_scan(mine);
   const int total = (int)lane_u32((uint32_t)upto, 63);
   d.share = deal.share(total, (int)wave_max((unsigned long long)longest));
-  d.c = blockIdx.x * d.share;
+  d.c = block * d.share;
   d.c_end = min(total, d.c + d.share);
   if (d.c >= d.c_end) return false;
   int l = __builtin_ctzll(__ballot(upto - mine <= d.c && d.c < upto));
@@ -126,20 +126,9 @@ __device__ __forceinline__ void deal_next(At at, Dealt &d) {
   do d.item = at(++d.i);
   while (d.item.chunks * d.item.subs == 0);
 }
-// Number of pieces of segment (i, sub) of `chunks` chunks, by every wave for itself.
-template <class At>
-__device__ __forceinline__ int deal_pieces(const Deal &deal, int n, At at, int i, int sub, int chunks) {
-  int total = 0, before = 0, longest = 0;
-  for (int u = 0; u < n; u += 64) {
-    const Segments s = at(min(u + lane_id(), n - 1));
-    const int all = u + lane_id() < n ? s.chunks * s.subs : 0;
-    total += all;
-    before += u + lane_id() < i ? all : 0;
-    longest = max(longest, s.chunks);
-  }
-  const int first = wave_sum(before) + sub * chunks;
-  const int share = deal.share(wave_sum(total), (int)wave_max((unsigned long long)longest));
-  return (first + chunks - 1) / share - first / share + 1;
+// Number of pieces of the segment.
+__device__ __forceinline__ int pieces_of(const Dealt &d) {
+  return (d.first + d.item.chunks - 1) / d.share - d.first / d.share + 1;
 }
 
 // ---- a call, as its kernels see it ----
@@ -151,6 +140,7 @@ constexpr int kDealtItems = 64 * 64;  // most sequences, or groups, that the loo
 struct Partials {
   float *acc;
   float2 *ml;
+  int32_t *pieces;   // per head, how many slots of either kind are in use (not written where there are no such rows)
   int32_t own, all;  // slots per head
 };
 

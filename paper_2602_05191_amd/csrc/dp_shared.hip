@@ -22,15 +22,11 @@
 // cores and the vector ALU have work of the same wave at the same time.
 // Blocks of 64 rows go global -> registers -> LDS, two blocks ahead of the products (three buffers, one barrier per block);
 // LDS rows are padded to 272 (keys) and 288 (values) bytes.
-#include "dp_attend.hpp"
-#include "dp_device.hpp"
-#include "dp_kernels.hpp"
-#include "dp_paged_rows.hpp"
+#include "dp_paged_body.hpp"
 
 namespace dp {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 *LdsTile;
@@ -51,7 +47,7 @@ __global__ __launch_bounds__(kSharedThreads) __attribute__((amdgpu_waves_per_eu(
   const int col_wave = wave / kParts, part = wave % kParts, half = lane >> 5;
   const PagedView &c = p.c;
   Dealt at;
-  if (!deal_start(p.shared, p.a.shared.n_groups, shared_segments(p), at)) return;
+  if (!deal_start(p.shared, blockIdx.x, p.a.shared.n_groups, shared_segments(p), at)) return;
 
   while (true) {
     const SharedGroup grp = shared_group(c, p.a.shared, at.i);
@@ -274,7 +270,10 @@ __global__ __launch_bounds__(kSharedThreads) __attribute__((amdgpu_waves_per_eu(
 
     if (busy && mine && part == 0) {
       const int64_t slot = head * p.parts.all + p.parts.own + split;
-      if (half == 0) p.parts.ml[slot] = make_float2(m, l);
+      if (half == 0) {
+        p.parts.ml[slot] = make_float2(m, l);
+        if (split == 0) p.parts.pieces[2 * head + 1] = pieces_of(at);
+      }
       float4 *dst = reinterpret_cast<float4 *>(p.parts.acc + slot * kHeadDim + 4 * half);
 #pragma unroll
       for (int n = 0; n < 4; ++n)
