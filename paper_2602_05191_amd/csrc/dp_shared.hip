@@ -22,13 +22,17 @@
 // cores and the vector ALU have work of the same wave at the same time.
 // Blocks of 64 rows go global -> registers -> LDS, two blocks ahead of the products (three buffers, one barrier per block);
 // LDS rows are padded to 272 (keys) and 288 (values) bytes.
-#include "dp_paged_body.hpp"
+#include "dp_attend.hpp"
+#include "dp_device.hpp"
+#include "dp_kernels.hpp"
+#include "dp_paged_rows.hpp"
 
 namespace dp {
 namespace {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) s16x4 *LdsTile;
 
 constexpr int kSharedWaves = 8, kSharedThreads = 64 * kSharedWaves;
