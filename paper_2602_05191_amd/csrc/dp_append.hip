@@ -47,6 +47,19 @@ __device__ __forceinline__ uint4 round8(const float (&x)[8]) {  // to nearest ev
   return __builtin_bit_cast(uint4, __builtin_convertvector(v, bf16x8));
 }
 
+// the r-th row of a token: keys, then values, then queries
+struct TokenRow {
+  int head;
+  bool is_v, is_q;
+};
+__device__ __forceinline__ TokenRow token_row(const PagedView &c, int r) {
+  TokenRow t;
+  t.is_v = r >= c.n_kv_heads && r < 2 * c.n_kv_heads;
+  t.is_q = r >= 2 * c.n_kv_heads;
+  t.head = t.is_q ? r - 2 * c.n_kv_heads : t.is_v ? r - c.n_kv_heads : r;
+  return t;
+}
+
 template <bool kF32>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView c, AppendTokens t, int parts) {
   __shared__ float2 s_turn[kAppendWaves][kHeadDim / 2];
@@ -55,6 +68,19 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView c, App
   const int64_t task = (int64_t)blockIdx.x * kAppendWaves + wave;
   const int token = (int)min(task / parts, (int64_t)t.n_tokens - 1), part = (int)(task % parts);
   bool live = task < (int64_t)t.n_tokens * parts;
+
+  // four rows per batch and wave; the first two batches are on their way while the token's place is found
+  const int rows = 2 * c.n_kv_heads + (t.q ? c.n_q_heads : 0), step = 4 * parts;
+  auto fetch = [&](int r, Slice<kF32> &s) {
+    const TokenRow row = token_row(c, min(r, rows - 1));
+    s.load(static_cast<const char *>(row.is_q ? t.q : row.is_v ? t.v : t.k) +
+               token * (row.is_q ? t.q_stride : row.is_v ? t.v_stride : t.k_stride) + row.head * (kHeadDim * (kF32 ? 4 : 2)),
+           t16);
+  };
+  int r = 4 * part + grp;
+  Slice<kF32> s0, s1;
+  fetch(r, s0);
+  fetch(r + step, s1);
 
   const int found = t.tok_ptr ? wave_find(t.tok_ptr, c.n_seqs, token) : token;
   live = live && found < c.n_seqs;
@@ -93,34 +119,40 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView c, App
   }
   const int partner = (lane & 48) + (!turns ? t16 : t16 < lanes_half ? t16 + lanes_half : t16 - lanes_half);
 
-  const int n_kv = c.n_kv_heads, rows = 2 * n_kv + (t.q ? c.n_q_heads : 0);
-  for (int r0 = 4 * part; r0 < rows; r0 += 4 * parts) {  // keys, values, queries
-    const int r = min(r0 + grp, rows - 1);
-    const bool is_v = r >= n_kv && r < 2 * n_kv, is_q = r >= 2 * n_kv;
-    const int head = is_q ? r - 2 * n_kv : is_v ? r - n_kv : r;
-    const char *src = static_cast<const char *>(is_q ? t.q : is_v ? t.v : t.k) +
-                      token * (is_q ? t.q_stride : is_v ? t.v_stride : t.k_stride) + head * (kHeadDim * (kF32 ? 4 : 2));
-    Slice<kF32> s;
-    s.load(src, t16);
+  auto finish = [&](int r, const Slice<kF32> &s) {
+    const TokenRow row = token_row(c, min(r, rows - 1));
     float x[8], y[8];
     s.widen(x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float other = t.adjacent ? x[e ^ 1] : __shfl(x[e], partner, 64);
       const float turned = fmaf(x[e], cosine[e], other * sine[e]);
-      y[e] = turns && !is_v ? turned : x[e];
+      y[e] = turns && !row.is_v ? turned : x[e];
     }
-    if (r0 + grp >= rows || (!is_q && !stored)) continue;
-    char *dst = is_q ? static_cast<char *>(t.q_out) + ((int64_t)token * c.n_q_heads + head) * kRowBytes
-                     : (is_v ? c.v_pages : c.k_pages) + place + head * c.head_stride;
+    if (r >= rows || (!row.is_q && !stored)) return;
+    char *dst = row.is_q ? static_cast<char *>(t.q_out) + ((int64_t)token * c.n_q_heads + row.head) * kRowBytes
+                         : (row.is_v ? c.v_pages : c.k_pages) + place + row.head * c.head_stride;
     reinterpret_cast<uint4 *>(dst)[t16] = round8(y);
+  };
+  for (int left = rows - 4 * part; left > 0; left -= 2 * step, r += 2 * step) {
+    Slice<kF32> n0, n1;
+    fetch(r + 2 * step, n0);
+    fetch(r + 3 * step, n1);
+    finish(r, s0);
+    finish(r + step, s1);
+    s0 = n0;
+    s1 = n1;
   }
 }
 
 }  // namespace
 
 hipError_t launch_append(const PagedView &c, const AppendTokens &t, hipStream_t s) {
-  const int parts = 1;
+  // A token's rows by one wave where there are enough tokens to fill the chip, else by several, down to four rows each: a
+  // call is then one round of loads.  us: one token of 48 rows 7.6 with one wave, 3.3 with twelve; 64 tokens 8.7 / 4.4.
+  constexpr int kChipWaves = 8192;
+  const int rows = 2 * c.n_kv_heads + (t.q ? c.n_q_heads : 0), most = (rows + 3) / 4, want = kChipWaves / t.n_tokens;
+  const int parts = want < 1 ? 1 : want < most ? want : most;
   const int64_t tasks = (int64_t)t.n_tokens * parts;
   const dim3 grid((unsigned)((tasks + kAppendWaves - 1) / kAppendWaves)), block(kAppendThreads);
   if (t.is_f32)
