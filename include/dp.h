@@ -436,10 +436,14 @@ typedef struct {
   int32_t max_group_seqs, max_shared_len; /* host-known bounds; max_shared_len <= the cache's max_seq_len */
   const int32_t *group_ptr;               /* [n_groups+1], ascending                                      */
   const int32_t *shared_lens;             /* [n_groups]; clamped to [0, max_shared_len]                   */
+  uint32_t flags;                         /* DP_SHARED_PREFIX_*                                           */
 } dp_shared_prefix;
 
 /* dp_paged_decode (all rows, no prior) with the shared rows of a group read once for all its sequences, through the
- * table of its first sequence that is long enough to hold them. */
+ * table of its first sequence that is long enough to hold them.  Where that would take longer (few sequences, few shared
+ * rows: the host decides by the bounds) every sequence is attended for itself, through its own table, unless
+ * DP_SHARED_PREFIX_ONCE is set. */
+#define DP_SHARED_PREFIX_ONCE 1u
 size_t dp_shared_prefix_workspace_bytes(const dp_paged_cache *cache, const dp_shared_prefix *prefix);
 dp_status dp_shared_prefix_decode(const dp_paged_cache *cache, const dp_shared_prefix *prefix, const void *q, void *out,
                                   dp_dtype out_dtype, float *lse, void *workspace, size_t workspace_bytes,

@@ -316,11 +316,12 @@ dp::PagedView view_of(const dp_paged_cache *c) {
 
 bool prefix_ok(const dp_paged_cache *c, const dp_shared_prefix *p) {
   return p && p->n_groups > 0 && p->max_group_seqs > 0 && p->max_shared_len >= 0 &&
-         p->max_shared_len <= c->max_seq_len && p->group_ptr && p->shared_lens;
+         p->max_shared_len <= c->max_seq_len && p->group_ptr && p->shared_lens && !(p->flags & ~DP_SHARED_PREFIX_ONCE);
 }
 
 dp::SharedView view_of(const dp_shared_prefix *p) {
-  return dp::SharedView{p->n_groups, p->max_group_seqs, p->max_shared_len, p->group_ptr, p->shared_lens};
+  return dp::SharedView{p->n_groups, p->max_group_seqs, p->max_shared_len, (p->flags & DP_SHARED_PREFIX_ONCE) != 0,
+                        p->group_ptr, p->shared_lens};
 }
 
 dp_status paged_attention(const dp_paged_cache *cache, const dp::PagedAttention &a, void *out, dp_dtype out_dtype,

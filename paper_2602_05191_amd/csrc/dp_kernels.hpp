@@ -155,6 +155,7 @@ hipError_t launch_append(const PagedView &c, const AppendTokens &t, hipStream_t 
 // Groups of sequences that begin with the same rows; n_groups == 0: none
 struct SharedView {
   int32_t n_groups, max_group_seqs, max_shared_len;
+  int32_t once;  // read them once whatever the sizes
   const int32_t *group_ptr, *shared_lens;
 };
 

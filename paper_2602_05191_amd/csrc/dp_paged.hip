@@ -387,7 +387,14 @@ Split split_of(const PagedView &c, const SharedView &shared) {
   // 10.0, of 768 11.3 / 9.9; 64 of 512 10.8 / 11.9, of 768 14.3 / 13.5; 128 of 768 15.7 / 15.7, of 1024 19.6 / 18.6; 256 of
   // 1536 33.4 / 38.1, ragged ones of up to 2048 36.0 / 34.2; 512 of 1024 43.2 / 48.0, ragged of up to 2048 67.6 / 63.6.
   s.whole = c.n_seqs > kDealtItems || c.max_seq_len <= (n_seg >= 256 ? 1536 : n_seg >= 128 ? 768 : 640);
-  const bool any_shared = shared.n_groups > 0 && shared.max_shared_len > 0 && shared.n_groups <= kDealtItems;
+  // Shared rows are read once where that saves more than 48 MiB of reads and 4 MiB per sequence: below, the launches that it
+  // takes cost more than the reads, which find much of what is shared in the caches.  us, shared once / every sequence for
+  // itself (G = 4, 8 KV heads, 100 rows of their own): 4 sequences, 4096 rows 22.4 / 21.6, 8192 rows 25.0 / 30.7; 16
+  // sequences, 1024 rows 22.1 / 19.8, 2048 rows 26.0 / 29.0; 64 sequences, 1024 rows 36.5 / 29.3, 2048 rows 42.1 / 53.7;
+  // 1 KV head: 64 sequences, 4096 rows 29.3 / 24.3, 8192 rows 33.6 / 42.2.
+  const long saved = ((long)c.n_seqs - shared.n_groups) * shared.max_shared_len * c.n_kv_heads * (2 * kRowBytes);
+  const bool any_shared = shared.n_groups > 0 && shared.max_shared_len > 0 && shared.n_groups <= kDealtItems &&
+                          (shared.once || saved > (48l << 20) + (4l << 20) * c.n_seqs);
   // one round of workgroups (two waves per SIMD x 256 CUs), and partial slots for some thousand pieces in all
   s.own.grid = at_least(at_most(n_seg * max_chunks, 2 * 256), 1);
   s.own.slots = s.whole ? 1 : at_least(at_most(max_chunks, at_most(at_least(16384 / nh, 8), kMaxSplits)), 1);

@@ -39,7 +39,7 @@ def append(**kw):
 
 
 def prefix(**kw):
-    base = dict(n_groups=1, max_group_seqs=4, max_shared_len=64, group_ptr=ONE, shared_lens=ONE)
+    base = dict(n_groups=1, max_group_seqs=4, max_shared_len=64, group_ptr=ONE, shared_lens=ONE, flags=0)
     base.update(kw)
     return B._SharedPrefix(**base)
 
@@ -98,7 +98,7 @@ def test_decodes_that_are_refused(lib):
 
 
 @pytest.mark.parametrize("bad", [dict(n_groups=0), dict(max_group_seqs=0), dict(max_shared_len=-1),
-                                 dict(max_shared_len=161), dict(group_ptr=None), dict(shared_lens=None)])
+                                 dict(max_shared_len=161), dict(group_ptr=None), dict(shared_lens=None), dict(flags=2)])
 def test_shared_prefixes_that_are_refused(lib, bad):
     c, p, one = C.byref(cache()), prefix(**bad), C.c_void_p(ONE)
     assert lib.dp_shared_prefix_decode(c, C.byref(p), one, one, 1, None, one, 1 << 40, None) == INVALID
