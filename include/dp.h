@@ -20,11 +20,13 @@
  *     or freed; the library keeps no state between calls that changes a result
  *     (it remembers per process how many workgroups of a kernel the device
  *     holds, asked from the runtime once, and dp_decode_attention_static owns a
- *     scratch array).  Inputs are never written.  Two calls that share a workspace must be ordered by the caller.
+ *     scratch array).  Inputs are never written (dp_append_kv writes the pages
+ *     of the cache it is given).  Two calls that share a workspace must be ordered by the caller.
  *   - Errors that can be detected on the host (null pointers, bad shapes, p out
  *     of range, workspace too small, unsupported head_dim) are returned before
  *     anything is launched.  Device data (offsets, sizes, ids) is NOT validated:
- *     out-of-range values there are undefined behaviour.
+ *     out-of-range values there are undefined behaviour (except where an entry
+ *     point says what they mean, as those over a paged cache do).
  *   - A "head" is a (sequence b, query head h) pair, index b*n_q_heads + h.  It
  *     reads KV segment seg = b*n_kv_heads + h/(n_q_heads/n_kv_heads).
  *   - Cluster ids in sel_ids are segment-local (0 .. Kc_seg-1).
@@ -42,7 +44,7 @@ extern "C" {
 typedef enum {
   DP_OK = 0,
   DP_ERR_INVALID_ARG = -1,         /* null pointer, non-positive shape, p outside its domain        */
-  DP_ERR_UNSUPPORTED = -2,         /* head_dim != 128, n_q_heads/n_kv_heads > 16, unknown dtype     */
+  DP_ERR_UNSUPPORTED = -2,         /* head_dim != 128, n_q_heads/n_kv_heads > 16, unknown dtype, sizes beyond a limit */
   DP_ERR_WORKSPACE_TOO_SMALL = -3, /* workspace_bytes < dp_workspace_bytes(problem)                 */
   DP_ERR_HIP = -4,                 /* a HIP runtime call failed (launch error)                      */
   DP_ERR_TOO_LARGE = -5            /* dp_decode_attention_static: dp_workspace_bytes(problem) > DP_STATIC_SCRATCH_BYTES */
@@ -365,7 +367,9 @@ dp_status dp_kmeans_fit(const dp_prefill *in, void *centroids, int32_t n_iters, 
  *   seq_lens    tokens of each sequence; larger values than max_seq_len are clamped to it, negative ones to 0
  *   page_table  an entry outside [0, n_pages) is a page that is not there: nothing is written to it, and its tokens
  *               are left out of attention.  Entries behind the last token of a sequence are not read.
- * Two sequences may share pages (dp_shared_prefix_decode). */
+ * Two sequences may share pages (dp_shared_prefix_decode).
+ * DP_ERR_UNSUPPORTED: head_dim != 128, a page_size that is no power of two, more than 2^22 sequences x query heads or 2^30
+ * rows of a sequence, strides that pass 2^30 elements inside a page. */
 typedef struct {
   int32_t n_seqs, n_kv_heads, n_q_heads, head_dim; /* n_q_heads % n_kv_heads == 0; head_dim == 128        */
   int32_t n_pages, page_size;                      /* page_size a power of two                            */
@@ -407,7 +411,7 @@ typedef struct {
 
 /* Stores the new tokens' keys (rotated) and values in the pages of the cache and the rotated queries in q_out.  Nothing
  * else of the pool is written.  Two tokens with the same place, or two sequences that append to one page's slot, leave
- * one of the two there.  Bitwise reproducible.  n_tokens == 0 does nothing. */
+ * one of the two there.  Bitwise reproducible.  n_tokens == 0 does nothing; DP_ERR_UNSUPPORTED above 2^25. */
 dp_status dp_append_kv(const dp_paged_cache *cache, const dp_kv_append *tokens, void *stream);
 
 /* Dense attention (Sec. 2.1, Eq. 1) of one query token per sequence over rows [first_rows[s], seq_lens[s]) of its pages
@@ -442,7 +446,7 @@ typedef struct {
 /* dp_paged_decode (all rows, no prior) with the shared rows of a group read once for all its sequences, through the
  * table of its first sequence that is long enough to hold them.  Where that would take longer (few sequences, few shared
  * rows: the host decides by the bounds) every sequence is attended for itself, through its own table, unless
- * DP_SHARED_PREFIX_ONCE is set. */
+ * DP_SHARED_PREFIX_ONCE is set; so it is with more than 4096 groups. */
 #define DP_SHARED_PREFIX_ONCE 1u
 size_t dp_shared_prefix_workspace_bytes(const dp_paged_cache *cache, const dp_shared_prefix *prefix);
 dp_status dp_shared_prefix_decode(const dp_paged_cache *cache, const dp_shared_prefix *prefix, const void *q, void *out,

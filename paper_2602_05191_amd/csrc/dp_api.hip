@@ -270,6 +270,8 @@ dp_status static_scratch(void **ptr) {
 constexpr int64_t kMaxPagedHeads = 1 << 22;  // sequences x query heads of a call (grid sizes stay below 2^32 threads)
 constexpr int32_t kMaxPagedLen = 1 << 30;    // rows of a sequence (a row number plus a round of tiles stays below 2^31)
 
+constexpr int32_t kMaxAppendTokens = 1 << 25;  // (the same)
+
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 dp_status paged_ok(const dp_paged_cache *c) {
@@ -703,7 +705,7 @@ dp_status dp_append_kv(const dp_paged_cache *cache, const dp_kv_append *tokens, 
   if (st != DP_OK) return st;
   if (!tokens || tokens->n_tokens < 0 || (tokens->flags & ~DP_ROPE_ADJACENT_PAIRS)) return DP_ERR_INVALID_ARG;
   if ((tokens->dtype != DP_BF16 && tokens->dtype != DP_F32) || tokens->rope_dims < 0 ||
-      tokens->rope_dims > dp::kHeadDim || tokens->rope_dims % 16)
+      tokens->rope_dims > dp::kHeadDim || tokens->rope_dims % 16 || tokens->n_tokens > kMaxAppendTokens)
     return DP_ERR_UNSUPPORTED;
   if (!tokens->tok_ptr && tokens->n_tokens != cache->n_seqs && tokens->n_tokens != 0) return DP_ERR_INVALID_ARG;
   if (tokens->n_tokens == 0) return DP_OK;

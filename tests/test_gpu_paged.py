@@ -198,6 +198,29 @@ def test_append_keys_and_values_only_and_queries_in_place(dp):
     assert np.array_equal(P.bits(other), P.bits(qd)) and P.turned_close(P.bits(qd), given, [32, 1, 6], f, False)
 
 
+def test_append_of_many_tokens_is_the_append_of_its_parts(dp):
+    """A prompt beyond 256 MiB of rows (written past the caches) and the same one in three parts (which are not): same bits."""
+    n, n_kv, n_q, page = 120000, 2, 6, 64
+    x = torch.randn(n, n_q + 2 * n_kv, 128, device="cuda", dtype=torch.bfloat16, generator=torch.Generator("cuda").manual_seed(1))
+    q, k, v = x[:, :n_q], x[:, n_q:n_q + n_kv], x[:, n_q + n_kv:]
+    f = torch.tensor(freqs_of(128), device="cuda")
+    table = torch.randperm(n // page, generator=torch.Generator().manual_seed(2)).int().cuda()[None]
+    results = []
+    for cuts in ([0, n], [0, 50000, 50001, n]):
+        pages = torch.zeros(2, n // page, n_kv, page, 128, device="cuda", dtype=torch.bfloat16)
+        lens = torch.zeros(1, device="cuda", dtype=torch.int32)
+        c = dp.PagedCache(pages[0], pages[1], table, lens, n, n_q)
+        out = torch.empty(n, n_q, 128, device="cuda", dtype=torch.bfloat16)
+        for a, b in zip(cuts, cuts[1:]):
+            lens.fill_(b)
+            dp.dp_append_kv(c, k[a:b], v[a:b], f, q=q[a:b], q_out=out[a:b], tok_ptr=up([0, b - a]))
+        results.append((pages, out))
+    torch.cuda.synchronize()
+    assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
+    at = [0, 77777, n - 1]
+    assert P.turned_close(P.bits(results[0][1][at]), P.wide(q[at]), at, freqs_of(128), False)
+
+
 def test_append_keeps_infinities_and_nan_in_their_pair(dp):
     lens, f = [5], freqs_of(64)
     for bad, dims in ((np.inf, (3, 35)), (np.nan, (3, 35)), (np.inf, (100,))):
@@ -350,6 +373,17 @@ def test_places_beyond_32_bits(dp):
     assert np.array_equal(got[:, 150 - 128], pool.k[pool.table[0, 2]][:, 150 - 128])
 
 
+@pytest.mark.parametrize("layout", ["head", "token"])
+def test_decode_of_very_many_sequences(dp, layout):
+    """More sequences than are dealt out (each is taken whole), some long, most short or empty."""
+    rng = np.random.default_rng(18)
+    lens = rng.integers(0, 24, 4200)
+    lens[[0, 99, 4199]] = 900, 1, 1300
+    pool = P.Pool(lens, 1, 16, seed=18)
+    q = queries(pool.rng, len(lens), 2)
+    P.check(paged(dp, pool, q, layout), P.decode(pool, q))
+
+
 # ------------------------------------------------------------ shared prefix --
 def shared_pool(ptr, shared, own_rows, n_kv, page, seed, idle=()):
     """Sequences of groups that begin alike: whole pages inside the shared rows are the same pages.  own_rows: rows of
@@ -432,6 +466,20 @@ def test_shared_prefix_is_the_paged_decode(dp):
     pool = shared_pool([0, 3, 9], [40, 100], own[:9], 2, 16, seed=25)
     q = queries(pool.rng, 9, 8)
     P.check(shared_decode(dp, pool, q, [-3, 3, 40], [40, 100], most=9), P.decode(pool, q))
+
+
+def test_shared_prefix_of_very_many_groups_and_sequences(dp):
+    """100 groups over 300 sequences, of which some share nothing; more groups than are dealt out."""
+    rng = np.random.default_rng(26)
+    ptr = np.concatenate([[0], np.sort(rng.integers(0, 301, 99)), [300]])
+    shared = rng.integers(0, 200, 100)
+    pool = shared_pool(ptr, shared, list(rng.integers(0, 50, 300)), 1, 16, seed=26, idle=set(rng.integers(0, 300, 20)))
+    q = queries(pool.rng, 300, 2)
+    P.check(shared_decode(dp, pool, q, ptr, shared), P.decode(pool, q))
+    pool = shared_pool(np.arange(4201), [16] * 4200, [3] * 4200, 1, 16, seed=27)
+    q = queries(pool.rng, 4200, 1)
+    P.check(shared_decode(dp, pool, q, np.arange(4201), [16] * 4200), P.decode(pool, q))
+    P.check(shared_decode(dp, pool, q, [0, 1, 4200], [16, 0]), P.decode(pool, q))
 
 
 def test_shared_prefix_without_rows(dp):
@@ -611,3 +659,16 @@ def test_bound_calls_and_streams(dp):
     torch.cuda.synchronize()
     for o, ref in zip(outs, refs):
         P.check(o, ref)
+    # two captured graphs, each with its own buffers, replayed in turn and at once
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    for (current, _), g in zip(calls, graphs):
+        with torch.cuda.graph(g):
+            current()
+    for _ in range(3):
+        for o, s, g in zip(outs, streams, graphs):
+            with torch.cuda.stream(s):
+                o[0].fill_(float("nan"))
+                g.replay()
+        torch.cuda.synchronize()
+        for o, ref in zip(outs, refs):
+            P.check(o, ref)

@@ -75,7 +75,7 @@ def test_caches_that_are_refused(lib, status, bad):
     (INVALID, dict(q_out=None)), (INVALID, dict(rope_freqs=None)), (INVALID, dict(flags=2)), (INVALID, dict(k=264)),
     (INVALID, dict(q=264)), (INVALID, dict(q_out=260)), (INVALID, dict(v_stride=-256)), (INVALID, dict(k_stride=260)),
     (INVALID, dict(q_stride=1 << 60)),
-    (UNSUPPORTED, dict(dtype=2)), (UNSUPPORTED, dict(rope_dims=8)), (UNSUPPORTED, dict(rope_dims=144)),
+    (UNSUPPORTED, dict(n_tokens=(1 << 25) + 1, tok_ptr=ONE)), (UNSUPPORTED, dict(dtype=2)), (UNSUPPORTED, dict(rope_dims=8)), (UNSUPPORTED, dict(rope_dims=144)),
     (UNSUPPORTED, dict(rope_dims=-16)),
 ])
 def test_appends_that_are_refused(lib, status, bad):
