@@ -132,7 +132,7 @@ __device__ __forceinline__ int pieces_of(const Dealt &d) {
 }
 
 // ---- a call, as its kernels see it ----
-constexpr int kSharedBlock = 64;       // shared rows per chunk
+constexpr int kSharedBlock = 64;       // shared rows that are attended between two barriers
 constexpr int kDealtItems = 64 * 64;  // most sequences, or groups, that the lookup of a share can hold
 
 // Partial results of a head: per slot the accumulator of its 128 dimensions, (maximum in base 2, sum).  The slots of its
@@ -188,12 +188,18 @@ __device__ __forceinline__ auto own_segments(const PagedArgs &p) {
   };
 }
 
+// Blocks of rows per chunk that is dealt out: a block takes the longer the more of the workgroup's waves have columns (1.4 us
+// with one to four, 2.9 with five).  Groups of 4, 13 and 20 sequences, G = 8, 20011 to 8545 rows: 72 us with one block for
+// all, 64 so.
+__device__ __forceinline__ int shared_blocks(int cols) { return cols <= 128 ? 2 : 1; }
+
 // groups; their KV heads, and of each the column tiles of a workgroup
 __device__ __forceinline__ auto shared_segments(const PagedArgs &p) {
   return [&p](int g) {
     const SharedGroup s = shared_group(p.c, p.a.shared, g);
-    const int tiles = ((s.end - s.begin) * p.c.group + p.shared_cols - 1) / p.shared_cols;
-    return Segments{(s.rows + kSharedBlock - 1) / kSharedBlock, p.c.n_kv_heads * tiles, s.begin, s.reader};
+    const int cols = (s.end - s.begin) * p.c.group, tiles = (cols + p.shared_cols - 1) / p.shared_cols;
+    const int rows = shared_blocks(cols) * kSharedBlock;
+    return Segments{(s.rows + rows - 1) / rows, p.c.n_kv_heads * tiles, s.begin, s.reader};
   };
 }
 

@@ -58,7 +58,8 @@ __global__ __launch_bounds__(kSharedThreads) __attribute__((amdgpu_waves_per_eu(
     const int tiles = at.item.subs / c.n_kv_heads, kv = at.sub / tiles;
     const int col0 = at.sub % tiles * p.shared_cols + kWaveCols * col_wave, n_cols = (grp.end - grp.begin) * c.group;
     const int split = blockIdx.x - at.first / at.share, seg_end = at.first + at.item.chunks;
-    const int block0 = at.c - at.first, block1 = min(at.c_end, seg_end) - at.first;
+    const int per = shared_blocks(n_cols), block0 = (at.c - at.first) * per;
+    const int block1 = min((min(at.c_end, seg_end) - at.first) * per, (grp.rows + kSharedBlock - 1) / kSharedBlock);
     const int32_t *table = c.table + (int64_t)grp.reader * c.table_stride;
     const bool busy = col0 < n_cols;
 
