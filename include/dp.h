@@ -419,7 +419,7 @@ dp_status dp_append_kv(const dp_paged_cache *cache, const dp_kv_append *tokens, 
  * What a step over the clustered prompt left (out and lse of dp_decode_attention in fp32) is joined where prior_out and
  * prior_lse are given (both or neither): the result is attention over both parts,
  *   out = (e^prior_lse prior_out + Z o) / (e^prior_lse + Z),  lse = ln(e^prior_lse + Z),
- * Z and o the normaliser and the output of the pages' rows.  prior_out may be out, prior_lse may be lse.
+ * Z and o the normaliser and the output of the pages' rows.  prior_out may be out (of fp32), prior_lse may be lse.
  *   q          bf16 [n_seqs, n_q_heads, head_dim], 16-byte aligned
  *   out, lse   as dp_sparse_decode; no row and no prior (prior_lse = -inf): out = 0, lse = -inf
  * Rows behind a sequence's last token (the rest of its last page) may hold anything, NaN included.
@@ -436,7 +436,7 @@ dp_status dp_paged_decode(const dp_paged_cache *cache, const void *q, const int3
  * max_group_seqs in its group share nothing: they are attended through their own table alone, as all others are behind
  * the shared rows. */
 typedef struct {
-  int32_t n_groups;
+  int32_t n_groups;                       /* at least 1                                                   */
   int32_t max_group_seqs, max_shared_len; /* host-known bounds; max_shared_len <= the cache's max_seq_len */
   const int32_t *group_ptr;               /* [n_groups+1], ascending                                      */
   const int32_t *shared_lens;             /* [n_groups]; clamped to [0, max_shared_len]                   */

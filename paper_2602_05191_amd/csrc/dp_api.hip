@@ -746,7 +746,9 @@ dp_status dp_paged_decode(const dp_paged_cache *cache, const void *q, const int3
   const dp_status st = paged_ok(cache);
   if (st != DP_OK) return st;
   if (out_dtype != DP_BF16 && out_dtype != DP_F32) return DP_ERR_UNSUPPORTED;
-  if (!q || !aligned16(q) || !out || !workspace || !prior_out != !prior_lse) return DP_ERR_INVALID_ARG;
+  if (!q || !aligned16(q) || !out || !workspace || !prior_out != !prior_lse ||
+      (prior_out && prior_out == out && out_dtype != DP_F32))
+    return DP_ERR_INVALID_ARG;
   if (workspace_bytes < dp_paged_workspace_bytes(cache)) return DP_ERR_WORKSPACE_TOO_SMALL;
   if (reinterpret_cast<uintptr_t>(workspace) % 256) return DP_ERR_INVALID_ARG;
   return paged_attention(cache, dp::PagedAttention{q, first_rows, prior_out, prior_lse, dp::SharedView{}}, out,

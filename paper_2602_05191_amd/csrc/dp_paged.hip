@@ -111,20 +111,21 @@ struct TileLoader {
   }
 };
 
-// ---- output of a head: partial results and what was known before, in base 2 ----
+// ---- output of a head: partial results and what was known before ----
+// (maxima as scaled scores: in base 2 the lowest numbers there are would pass the range)
 struct Merged {
   float m, l, o;  // maximum, sum, accumulator of one dimension
 };
-__device__ __forceinline__ void store_head(const PagedArgs &p, int64_t head, int d, float prior_lse, float prior_o, Merged x) {
-  const float prior = prior_lse * kLog2e;
+__device__ __forceinline__ float weight_of(float m, float sub) { return exp2f((m - sub) * kLog2e); }
+__device__ __forceinline__ void store_head(const PagedArgs &p, int64_t head, int d, float prior, float prior_o, Merged x) {
   const float M = fmaxf(x.m, prior), sub = finite_max(M);
-  const float w = exp2f(x.m - sub), wp = exp2f(prior - sub);
+  const float w = weight_of(x.m, sub), wp = weight_of(prior, sub);
   const float L = fmaf(x.l, w, wp);
   float o = x.m > -INFINITY ? x.o * w : 0.f;
   if (prior > -INFINITY) o = fmaf(prior_o, wp, o);  // (a prior without weight may hold anything)
   const bool any = L > 0.f;
   store_out(p.attn.out, p.attn.out_is_bf16, head, d, any ? o / L : 0.f);
-  if (p.attn.lse && d == 0) p.attn.lse[head] = any ? (M + log2f(L)) * kLn2 : -INFINITY;
+  if (p.attn.lse && d == 0) p.attn.lse[head] = any ? fmaf(log2f(L), kLn2, M) : -INFINITY;
 }
 
 template <bool kSmallPages, bool kShared>
@@ -257,7 +258,7 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
     // merge the waves through LDS: lane (r, kq) holds dims 8 (4 kq + i) + n of head r
     if (r < n_live) {
       if (kq == 0) {
-        s_m[wave][r] = m * p.scale_log2;
+        s_m[wave][r] = m * p.c.sm_scale;
         s_l[wave][r] = l;
       }
 #pragma unroll
@@ -282,7 +283,7 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
       for (int w = 0; w < kPagedWaves; ++w) x.m = fmaxf(x.m, s_m[w][j]);
 #pragma unroll
       for (int w = 0; w < kPagedWaves; ++w) {
-        const float wg = (s_m[w][j] == -INFINITY) ? 0.f : exp2f(s_m[w][j] - x.m);
+        const float wg = weight_of(s_m[w][j], finite_max(x.m));
         x.l += s_l[w][j] * wg;
         x.o += s_acc[w][j][d] * wg;
       }
@@ -336,12 +337,12 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(PagedArgs p) {
       if (s0 + kGroups * u >= n_active) ml[u] = make_float2(-INFINITY, 0.f);
       top = fmaxf(top, ml[u].x);
     }
-    const float sub = finite_max(top), sc = exp2f(m - sub);
+    const float sub = finite_max(top), sc = weight_of(m, sub);
     l *= sc;
     o.x *= sc; o.y *= sc; o.z *= sc; o.w *= sc;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      const float w = exp2f(ml[u].x - sub);
+      const float w = weight_of(ml[u].x, sub);
       l = fmaf(ml[u].y, w, l);
       if (s0 + kGroups * u < n_active) {
         o.x = fmaf(oo[u].x, w, o.x);
@@ -364,7 +365,7 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(PagedArgs p) {
   for (int v = 1; v < kGroups; ++v) all.m = fmaxf(all.m, s_m[v]);
 #pragma unroll
   for (int v = 0; v < kGroups; ++v) {
-    const float w = exp2f(s_m[v] - finite_max(all.m));
+    const float w = weight_of(s_m[v], finite_max(all.m));
     all.l = fmaf(s_l[v], w, all.l);
     all.o = fmaf(s_o[v][threadIdx.x], w, all.o);
   }
@@ -392,7 +393,7 @@ Split split_of(const PagedView &c, const SharedView &shared) {
   // itself (G = 4, 8 KV heads, 100 rows of their own): 4 sequences, 4096 rows 22.4 / 21.6, 8192 rows 25.0 / 30.7; 16
   // sequences, 1024 rows 22.1 / 19.8, 2048 rows 26.0 / 29.0; 64 sequences, 1024 rows 36.5 / 29.3, 2048 rows 42.1 / 53.7;
   // 1 KV head: 64 sequences, 4096 rows 29.3 / 24.3, 8192 rows 33.6 / 42.2.
-  const long saved = ((long)c.n_seqs - shared.n_groups) * shared.max_shared_len * c.n_kv_heads * (2 * kRowBytes);
+  const long saved = ((long)c.n_seqs - at_most(shared.n_groups, kDealtItems)) * shared.max_shared_len * c.n_kv_heads * (2 * kRowBytes);
   const bool any_shared = shared.n_groups > 0 && shared.max_shared_len > 0 && shared.n_groups <= kDealtItems &&
                           (shared.once || saved > (48l << 20) + (4l << 20) * c.n_seqs);
   // one round of workgroups (two waves per SIMD x 256 CUs), and partial slots for some thousand pieces in all

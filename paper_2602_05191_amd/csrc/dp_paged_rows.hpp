@@ -135,7 +135,7 @@ __device__ __forceinline__ int pieces_of(const Dealt &d) {
 constexpr int kSharedBlock = 64;       // shared rows that are attended between two barriers
 constexpr int kDealtItems = 64 * 64;  // most sequences, or groups, that the lookup of a share can hold
 
-// Partial results of a head: per slot the accumulator of its 128 dimensions, (maximum in base 2, sum).  The slots of its
+// Partial results of a head: per slot the accumulator of its 128 dimensions, (maximum, sum).  The slots of its
 // own rows come first, then those of the rows that it shares.
 struct Partials {
   float *acc;

@@ -250,7 +250,7 @@ __global__ __launch_bounds__(kSharedThreads) __attribute__((amdgpu_waves_per_eu(
       now = next;
     }
     l += xor32(l);
-    m *= p.scale_log2;
+    m *= c.sm_scale;
 
     if constexpr (kParts == 2) {  // the two halves of the rows meet in LDS
       float *slot = reinterpret_cast<float *>(&s_rows[0][0]) + col_wave * (66 * 64) + lane;
@@ -264,7 +264,7 @@ __global__ __launch_bounds__(kSharedThreads) __attribute__((amdgpu_waves_per_eu(
       __syncthreads();
       if (part == 0) {
         const float mo = slot[64 * 64], top = fmaxf(m, mo), sub = finite_max(top);
-        const float w = __builtin_amdgcn_exp2f(m - sub), wo = __builtin_amdgcn_exp2f(mo - sub);
+        const float w = __builtin_amdgcn_exp2f((m - sub) * kLog2e), wo = __builtin_amdgcn_exp2f((mo - sub) * kLog2e);
         l = fmaf(l, w, slot[65 * 64] * wo);
 #pragma unroll
         for (int i = 0; i < 64; ++i) O[i / 16][i % 16] = fmaf(O[i / 16][i % 16], w, slot[i * 64] * wo);

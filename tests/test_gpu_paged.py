@@ -344,6 +344,33 @@ def test_decode_rows_that_are_masked_by_their_score(dp, low, n, lo, hi):
     P.check(paged(dp, pool, q), P.decode(pool, q))
 
 
+LOWEST = float(P.wide(np.array(H_LOWEST)))
+
+
+def only_dim_7(pool, q, scores):
+    """Keys and queries so that row i of every sequence scores exactly scores(i) at sm_scale = 1."""
+    q[:], q[..., 7] = 0, H_ONE
+    there = ~np.isnan(P.wide(pool.k))
+    pool.k[there] = 0
+    for s, n in enumerate(pool.lens):
+        i = np.arange(n)
+        pool.k[pool.table[s, i // pool.page], :, i % pool.page, 7] = P.to_bf16_bits(scores(i))[:, None]
+
+
+@pytest.mark.parametrize("prior", [False, True])
+@pytest.mark.parametrize("n", [37, 3000])
+def test_decode_of_rows_that_score_the_lowest_numbers(dp, n, prior):
+    """All rows at the lowest number there is: the mean; the lesser of two such scores has no weight (both forms)."""
+    for scores in (lambda i: np.full(len(i), LOWEST), lambda i: np.where(i % 3 == 0, LOWEST, -2.0 ** 127)):
+        pool = P.Pool([n, 11], 1, 16, seed=41)
+        q = queries(pool.rng, 2, 4)
+        only_dim_7(pool, q, scores)
+        kw = {}
+        if prior:
+            kw["prior"] = pool.rng.standard_normal((2, 4, 128)).astype(np.float32), np.full((2, 4), LOWEST, np.float32)
+        P.check(paged(dp, pool, q, sm_scale=1.0, **kw), P.decode(pool, q, scale=1.0, **kw))
+
+
 def test_decode_sm_scale(dp):
     pool = P.Pool([333, 20], 1, 16, seed=16)
     q = queries(pool.rng, 2, 3)
@@ -402,9 +429,10 @@ def shared_pool(ptr, shared, own_rows, n_kv, page, seed, idle=()):
     return pool
 
 
-def shared_decode(dp, pool, q, ptr, shared, most=None, longest=None, layout="head", dtype=torch.float32, max_len=None, once=True):
+def shared_decode(dp, pool, q, ptr, shared, most=None, longest=None, layout="head", dtype=torch.float32, max_len=None, once=True,
+                  sm_scale=0.0):
     """once: the shared rows read once whatever the sizes (small calls attend every sequence for itself)."""
-    c = pool.device(q.shape[1], layout, max_len)
+    c = pool.device(q.shape[1], layout, max_len, sm_scale)
     most = int(max(np.diff(ptr).max(), 1)) if most is None else most
     prefix = dp.SharedPrefix(up(ptr), up(shared), most, int(max(max(shared), 0)) if longest is None else longest,
                              dp.DP_SHARED_PREFIX_ONCE if once else 0)
@@ -517,6 +545,15 @@ def test_shared_prefix_keeps_what_is_not_finite_in_its_place(dp, dtype):
             pool.v[pool.table[0, 250 // 16], 0, 250 % 16, 5] = H_INF
             out, _ = shared_decode(dp, pool, q, [0, 9], [300], dtype=dtype)
             assert torch.isposinf(out[..., 5]).all() and torch.isfinite(out).sum() == out.numel() - 9 * 4
+
+
+@pytest.mark.parametrize("n_seqs", [9, 40])
+def test_shared_rows_that_score_the_lowest_numbers(dp, n_seqs):
+    for scores in (lambda i: np.full(len(i), LOWEST), lambda i: np.where(i < 64, LOWEST, -2.0 ** 127)):
+        pool = shared_pool([0, n_seqs], [304], [20] * n_seqs, 1, 16, seed=42)
+        q = queries(pool.rng, n_seqs, 4)
+        only_dim_7(pool, q, scores)
+        P.check(shared_decode(dp, pool, q, [0, n_seqs], [304], sm_scale=1.0), P.decode(pool, q, scale=1.0))
 
 
 # ------------------------------------------------------------ used together --

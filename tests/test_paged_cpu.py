@@ -97,6 +97,13 @@ def test_decodes_that_are_refused(lib):
     assert call(n=lib.dp_paged_workspace_bytes(c) - 1) == SMALL
 
 
+def test_a_prior_of_fp32_is_not_joined_in_place_of_bf16(lib):
+    c, one, other = C.byref(cache()), C.c_void_p(ONE), C.c_void_p(2 * ONE)
+    call = lambda out, dt: lib.dp_paged_decode(c, one, None, other, other, out, dt, None, one, 0, None)  # noqa: E731
+    bf16, fp32 = 0, 1
+    assert call(other, bf16) == INVALID and call(one, bf16) == SMALL and call(other, fp32) == SMALL
+
+
 @pytest.mark.parametrize("bad", [dict(n_groups=0), dict(max_group_seqs=0), dict(max_shared_len=-1),
                                  dict(max_shared_len=161), dict(group_ptr=None), dict(shared_lens=None), dict(flags=2)])
 def test_shared_prefixes_that_are_refused(lib, bad):
