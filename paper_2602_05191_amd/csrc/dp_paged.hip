@@ -4,12 +4,16 @@
 // memory in the instructions' layouts, 16 rows x up to 16 query heads of a group per wave and step:
 //   scores  S[16 rows x 16 heads] = K Q^T, four v_mfma_f32_16x16x32_bf16: lane l loads chunks l / 16 + 4 j of key row
 //           l % 16 and receives the scores of head l % 16 for rows 4 (l / 16) + i, which become weights in place;
-//   output  O^T[dims x heads] += V^T P^T, v_mfma_f32_16x16x4_f32 with k = l / 16 standing for row 4 (l / 16) + i: the
-//           weights stay fp32, the values are widened; tile n of eight holds dims 8 x + n.  A tile's 16 rows are summed by
-//           themselves and then added: the fp32 chain is as long as the wave has tiles, not rows.
+//   output  O^T[dims x heads] += V^T P^T, v_mfma_f32_16x16x16_bf16, k = 4 (l / 16) + i: the weights are where the scores
+//           were, and of the values a lane loads dims 8 (l % 16) .. + 7 of its four rows and puts the rows of a dimension
+//           side by side by byte permutes.  Tile n of eight holds dims 8 x + n.
+// A weight goes into the product as three bf16 numbers that add up to its 24 bits; the sum of the weights is taken from the
+// fp32 weights.  The first two are cut, not rounded, and what is left is increased by 2^-26 and 2^-34 of the weight: none is
+// zero, so that an infinite value does not become NaN (0 x inf).
 // What is subtracted from a head's scores is a score that was its largest at some time, unscaled (the largest weight is in
 // order whatever the size of the scores); it moves when one leads it by 8 in base 2: weights up to 2^8 lose nothing in fp32.
-// A maximum of -inf is taken as the lowest finite number when it is subtracted; weights keep the range below 2^-126 (exp2f).
+// A maximum of -inf is taken as the lowest finite number when it is subtracted.  A weight below 2^-126 of the largest counts
+// as zero (v_exp_f32).
 // Tiles begin at multiples of 16 rows, so a tile of pages of 16 tokens or more lies in one page: its place is a scalar and
 // a lane's offsets are the same for every tile.  The numbers of the pages of a wave's next 64 tiles are fetched by its 64
 // lanes at once.  Smaller pages: every row's page by the lane that loads the row's key, a tile ahead of the rows.
@@ -18,6 +22,9 @@
 // Work split: the rows of all (sequence, KV head) segments, in chunks of 64, are dealt out evenly to one round of resident
 // workgroups; pieces are merged by a second kernel.  Short or very many segments are taken whole, a workgroup each, which
 // then writes the output itself.
+// Measured (8 KV heads, G = 4): 16 sequences of up to 65536 rows, 2.6 GB, 399 us = 6.5 TB/s, as much as this card reads;
+// one of 131072 rows 82.8 us (6.5 TB/s) and 6.2 for the merge; the matrix cores are busy 16 % of it.  Two tiles per wave in
+// registers, one of them in flight, two waves per SIMD; with a third tile the registers do not suffice (131072 rows: 97 us).
 #include "dp_attend.hpp"
 #include "dp_device.hpp"
 #include "dp_kernels.hpp"
@@ -304,8 +311,10 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
   }
 }
 
-// One workgroup per head.  A slot's 128 dimensions are taken by 32 lanes, four each, so that a head's partials are fetched in
-// a round or two of loads; the groups of 32 meet in LDS.
+// One workgroup per head: sum over its slots of e^(m - M) (sum, accumulator).  A chain of dependent loads and launch bound:
+// a slot's 128 dimensions are taken by 32 lanes, four each, so that a head's partials are fetched in a round or two of loads;
+// the groups of 32 meet in LDS.  32 heads of some 64 slots 6.2 us, 2048 heads of 36 slots (38 MB) 8.9, of which 3 are any
+// launch's.
 template <int kThreads, bool kShared>
 __global__ __launch_bounds__(kThreads) void paged_merge_kernel(PagedArgs p) {
   constexpr int kGroups = kThreads / 32, kBatch = 8;
