@@ -411,6 +411,67 @@ def test_decode_of_very_many_sequences(dp, layout):
     P.check(paged(dp, pool, q, layout), P.decode(pool, q))
 
 
+@pytest.mark.parametrize("form", ["wide_table", "no_lse", "odd_out", "raw_bits"])
+def test_forms_of_arguments(dp, form):
+    """A table that is a slice of a wider one; no lse; an output at an odd element; queries and pages as raw bits."""
+    pool = P.Pool([3000, 0, 70], 2, 16, seed=43)
+    q = queries(pool.rng, 3, 8)
+    c, Q = pool.device(8), q_dev(q)
+    if form == "wide_table":
+        wide = torch.full((3, c.page_table.shape[1] + 9), 1 << 30, dtype=torch.int32, device="cuda")
+        table = wide[:, 4:4 + c.page_table.shape[1]]
+        table.copy_(c.page_table)
+        c = dp.PagedCache(c.k_pages, c.v_pages, table, c.seq_lens, 3000, 8)
+    if form == "raw_bits":
+        Q = Q.view(torch.int16)
+    else:
+        c = dp.PagedCache(c.k_pages.view(torch.bfloat16), c.v_pages.view(torch.bfloat16), c.page_table, c.seq_lens, 3000, 8)
+    dtype = torch.bfloat16 if form == "odd_out" else torch.float32
+    out = torch.full((3 * 8 * 128 + 1,), float("nan"), dtype=dtype, device="cuda")[1:].view(3, 8, 128)
+    lse = None if form == "no_lse" else torch.empty(3, 8, device="cuda")
+    ref = P.decode(pool, q)
+    prefix = dp.SharedPrefix(up([0, 1]), up([100]), 1, 100, dp.DP_SHARED_PREFIX_ONCE)
+    for call, n in ((dp.dp_paged_decode, dp.dp_paged_workspace_bytes(c)),
+                    (dp.dp_shared_prefix_decode, dp.dp_shared_prefix_workspace_bytes(c, prefix))):
+        ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+        out.fill_(float("nan"))
+        call(c, *([prefix] if call is dp.dp_shared_prefix_decode else []), Q, out, lse, ws)
+        torch.cuda.synchronize()
+        P.check((out, torch.from_numpy(ref[1]) if lse is None else lse), ref, dtype)
+
+
+def test_a_pool_without_pages(dp):
+    """Nothing is stored, nothing read; the prior passes through, queries are rotated."""
+    pages = torch.empty(0, 2, 16, 128, dtype=torch.bfloat16, device="cuda")
+    c = dp.PagedCache(pages, pages, torch.zeros(2, 4, dtype=torch.int32, device="cuda"), up([64, 3]), 64, 4)
+    rng = np.random.default_rng(44)
+    q = queries(rng, 2, 4)
+    prior = torch.randn(2, 4, 128, device="cuda"), torch.randn(2, 4, device="cuda")
+    b = Buffers(2, 4, dp.dp_paged_workspace_bytes(c))
+    dp.dp_paged_decode(c, q_dev(q), b.out.t, b.lse.t, b.ws.t, prior_out=prior[0], prior_lse=prior[1])
+    out, lse = b.done()
+    # one weight, 2^(lse - lse): out = o / 1, lse = lse + ln 1
+    assert torch.equal(out, prior[0]) and torch.equal(lse, prior[1])
+    k, turned = q_dev(queries(rng, 2, 2)), torch.empty(2, 4, 128, dtype=torch.bfloat16, device="cuda")
+    dp.dp_append_kv(c, k, k, q=q_dev(q), q_out=turned)
+    torch.cuda.synchronize()
+    assert np.array_equal(P.bits(turned), q)
+
+
+def test_append_of_one_row_for_all(dp):
+    """Keys and values with a stride of zero between tokens."""
+    pool = P.Pool([0], 2, 16, seed=45, width=3, spare=40)
+    k = torch.from_numpy(pool.rng.standard_normal((1, 2, 128))).float().cuda().expand(37, 2, 128)
+    pool.lens[:] = 37
+    c = pool.device(4)
+    dp.dp_append_kv(c, k, k, tok_ptr=up([0, 37]))
+    torch.cuda.synchronize()
+    want = P.to_bf16_bits(k[0].cpu().numpy())
+    for i in range(37):
+        for pages in (c.k_pages, c.v_pages):
+            assert np.array_equal(P.bits(pages[int(pool.table[0, i // 16]), :, i % 16]), want)
+
+
 # ------------------------------------------------------------ shared prefix --
 def shared_pool(ptr, shared, own_rows, n_kv, page, seed, idle=()):
     """Sequences of groups that begin alike: whole pages inside the shared rows are the same pages.  own_rows: rows of
