@@ -21,10 +21,12 @@
 // values are made zero: they may hold anything.
 // Work split: the rows of all (sequence, KV head) segments, in chunks of 64, are dealt out evenly to one round of resident
 // workgroups; pieces are merged by a second kernel.  Short or very many segments are taken whole, a workgroup each, which
-// then writes the output itself.
-// Measured (8 KV heads, G = 4): 16 sequences of up to 65536 rows, 2.6 GB, 399 us = 6.5 TB/s, as much as this card reads;
-// one of 131072 rows 82.8 us (6.5 TB/s) and 6.2 for the merge; the matrix cores are busy 16 % of it.  Two tiles per wave in
-// registers, one of them in flight, two waves per SIMD; with a third tile the registers do not suffice (131072 rows: 97 us).
+// then writes the output itself.  Where the heads of a token lie side by side a workgroup's waves take the same rows of four
+// KV heads (chunks of 16 rows), not a head's rows in turn: what lies next to each other is read at one time.
+// Measured (8 KV heads, G = 4): 16 sequences of up to 65536 rows, 2.6 GB, 399 us = 6.5 TB/s, as much as this card reads (the
+// matrix cores are busy 16 % of it); one of 131072 rows 82.8 us (6.5 TB/s) and 6.2 for the merge; heads side by side, G = 8,
+// four of 131072 rows 332 us (6.5 TB/s; 372 with a head per workgroup).  Two tiles per wave in registers, one of them in
+// flight, two waves per SIMD; with a third tile the registers do not suffice (131072 rows: 97 us).
 #include "dp_attend.hpp"
 #include "dp_device.hpp"
 #include "dp_kernels.hpp"
@@ -51,9 +53,8 @@ struct PagedTile {
 };
 
 // Fetches tiles of one segment: rows t .. t + 15, t a multiple of 16, of the wave's tiles t0, t0 + kStep, ...
-template <bool kSmallPages>
+template <bool kSmallPages, int kStep>
 struct TileLoader {
-  static constexpr int kStep = kPagedWaves * kPagedTile;
   const PagedView &c;
   const int32_t *table;      // of the sequence
   const char *k, *v;         // of the KV head
@@ -135,22 +136,23 @@ __device__ __forceinline__ void store_head(const PagedArgs &p, int64_t head, int
   if (p.attn.lse && d == 0) p.attn.lse[head] = any ? fmaf(log2f(L), kLn2, M) : -INFINITY;
 }
 
-template <bool kSmallPages, bool kShared>
+template <bool kSmallPages, bool kShared, int kSpan>
 __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_kernel(PagedArgs p) {
   __shared__ float s_m[kPagedWaves][kPagedHeads], s_l[kPagedWaves][kPagedHeads], s_prior[kPagedHeads];
   __shared__ __align__(16) float s_acc[kPagedWaves][kPagedHeads][kHeadDim + 4];
   const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
   const int r = lane & 15, kq = lane >> 4;
+  constexpr int kRows = own_chunk(kSpan);
   const int n_kv = p.c.n_kv_heads, group = p.c.group, n_live = min(kPagedHeads, group - p.head0);
   Dealt at;
   if (p.whole) {
     at.i = blockIdx.x / n_kv;
     at.sub = blockIdx.x % n_kv;
-    at.item = own_segments<kShared>(p)(at.i);
+    at.item = own_segments<kShared, kSpan>(p)(at.i);
     at.first = at.c = 0;
     at.c_end = at.item.chunks;
     at.share = 1;
-  } else if (!deal_start(p.own, blockIdx.x, p.c.n_seqs, own_segments<kShared>(p), at)) {
+  } else if (!deal_start(p.own, blockIdx.x, p.c.n_seqs, own_segments<kShared, kSpan>(p), at)) {
     return;
   }
 
@@ -158,10 +160,11 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
   while (true) {
     const SeqRows rows{at.item.a, at.item.b};
     const int seg_end = at.first + at.item.chunks;
-    const int ra = (rows.chunk0() + at.c - at.first) * kChunkRows;
-    const int rb = min(rows.len, (rows.chunk0() + min(at.c_end, seg_end) - at.first) * kChunkRows);
+    const int ra = (rows.first / kRows + at.c - at.first) * kRows;
+    const int rb = min(rows.len, (rows.first / kRows + min(at.c_end, seg_end) - at.first) * kRows);
     const int split = p.whole ? 0 : blockIdx.x - at.first / at.share;  // number of the piece inside its segment
-    const int64_t head_first = (int64_t)at.i * p.c.n_q_heads + at.sub * group + p.head0;
+    const int kv = kSpan == 1 ? at.sub : at.sub * kSpan + wave;
+    const int64_t head_first = (int64_t)at.i * p.c.n_q_heads + kv * group + p.head0;
 
     // query head r of the pass (beyond the group: its last head again, not stored), chunks kq + 4 j
     uint4 Q[4];
@@ -234,10 +237,10 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
       }
     };
 
-    // the workgroup's waves take tiles in turn; the next tile's loads are in flight during a tile's arithmetic
-    TileLoader<kSmallPages> tiles(p.c, at.i, at.sub, rows);
-    constexpr int kStep = kPagedWaves * kPagedTile;
-    int t = ra + wave * kPagedTile;
+    // the workgroup's waves take tiles in turn, or a KV head each; the next tile's loads are in flight during a tile's arithmetic
+    constexpr int kStep = kSpan == 1 ? kPagedWaves * kPagedTile : kPagedTile;
+    TileLoader<kSmallPages, kStep> tiles(p.c, at.i, kv, rows);
+    int t = kSpan == 1 ? ra + wave * kPagedTile : ra;
     if (t < rb) {
       PagedTile d0, d1;
       tiles.start(t);
@@ -275,15 +278,25 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
         dst[1] = make_float4(acc[4][i], acc[5][i], acc[6][i], acc[7][i]);
       }
     }
-    const bool direct = !kShared && p.whole;
-    if (!kShared) {  // (read before any of it may be overwritten)
+    const bool direct = kSpan == 1 && !kShared && p.whole;
+    if (kSpan == 1 && !kShared) {  // (read before any of it may be overwritten)
       if (tid < n_live) s_prior[tid] = direct && p.a.prior_lse ? p.a.prior_lse[head_first + tid] : -INFINITY;
     }
     __syncthreads();
+    if constexpr (kSpan > 1) {  // a KV head per wave: nothing to merge
+      for (int j = 0; j < n_live; ++j) {
+        const int64_t slot = (head_first + j) * p.parts.all + split;
+        reinterpret_cast<float2 *>(p.parts.acc + slot * kHeadDim)[lane] = reinterpret_cast<const float2 *>(s_acc[wave][j])[lane];
+        if (lane == 0) {
+          p.parts.ml[slot] = make_float2(s_m[wave][j], s_l[wave][j]);
+          if (split == 0) p.parts.pieces[2 * (head_first + j)] = pieces_of(at);
+        }
+      }
+    }
     // thread t: dim t % 128 of heads t / 128, t / 128 + 2, ...
     const int d = tid % kHeadDim;
 #pragma unroll 2
-    for (int j = tid / kHeadDim; j < n_live; j += kPagedThreads / kHeadDim) {
+    for (int j = tid / kHeadDim; kSpan == 1 && j < n_live; j += kPagedThreads / kHeadDim) {
       const float prior_o = direct && p.a.prior_lse ? p.a.prior_out[(head_first + j) * kHeadDim + d] : 0.f;
       Merged x{-INFINITY, 0.f, 0.f};
 #pragma unroll
@@ -307,7 +320,7 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
     }
     if (seg_end >= at.c_end) break;
     __syncthreads();  // LDS is reused by the next piece
-    deal_next(own_segments<kShared>(p), at);
+    deal_next(own_segments<kShared, kSpan>(p), at);
   }
 }
 
@@ -325,7 +338,7 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(PagedArgs p) {
   const float prior_lse = p.a.prior_lse ? p.a.prior_lse[head] : -INFINITY;
   const float prior_o = p.a.prior_lse && threadIdx.x < kHeadDim ? p.a.prior_out[(int64_t)head * kHeadDim + threadIdx.x] : 0.f;
   const SeqRows rows = seq_rows<kShared>(p, head / p.c.n_q_heads);
-  const int n_own = rows.chunks() > 0 || p.whole ? pieces.x : 0;
+  const int n_own = rows.first < rows.len || p.whole ? pieces.x : 0;
   const int n_active = n_own + (kShared && rows.first > 0 ? pieces.y : 0);
   const int64_t slot0 = (int64_t)head * p.parts.all;
   float m = -INFINITY, l = 0.f;
@@ -383,7 +396,7 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(PagedArgs p) {
 
 // How a call is split; by sizes that the host knows.
 struct Split {
-  int whole, cols;  // own rows; shared rows: columns of a workgroup
+  int whole, span, cols;  // own rows; shared rows: columns of a workgroup
   Deal own, shared;
 };
 int at_most(long n, long most) { return (int)(n < most ? n : most); }
@@ -405,9 +418,21 @@ Split split_of(const PagedView &c, const SharedView &shared) {
   const long saved = ((long)c.n_seqs - at_most(shared.n_groups, kDealtItems)) * shared.max_shared_len * c.n_kv_heads * (2 * kRowBytes);
   const bool any_shared = shared.n_groups > 0 && shared.max_shared_len > 0 && shared.n_groups <= kDealtItems &&
                           (shared.once || saved > (48l << 20) + (4l << 20) * c.n_seqs);
+  // Where the heads of a token lie side by side (pages with the tokens outermost) a workgroup takes the same rows of four
+  // heads, a wave each: 1 KB next to each other, and neighbouring workgroups the rest, where waves of one head alone read
+  // 256 bytes here and there.  us, a head per workgroup / four (8 KV heads, G = 4): 16 sequences of up to 65536 rows 450 /
+  // 397, one of 131072 102 / 92, of 32768 33.4 / 31.7, 64 of 2048 99 / 91.  Shorter, the steps of a wave are too few and the
+  // pieces to merge too many: one of 8192 16.7 / 17.3, four of 4096 20.1 / 21.5; 4 KV heads, one of 65536 30.8 / 32.1.
+  // (Behind shared rows: by the rows beyond them.)
+  const int own_chunks = max_chunks - (any_shared ? shared.max_shared_len / kChunkRows : 0);
+  const bool heads_together = c.head_stride < (c.page_shift ? (int64_t)c.slot_stride : c.page_stride);
+  s.span = !s.whole && heads_together && c.n_kv_heads % kPagedWaves == 0 && n_seg >= 2 * kPagedWaves && n_seg * own_chunks >= 4096
+               ? kPagedWaves : 1;
   // one round of workgroups (two waves per SIMD x 256 CUs), and partial slots for some thousand pieces in all
   s.own.grid = at_least(at_most(n_seg * max_chunks, 2 * 256), 1);
-  s.own.slots = s.whole ? 1 : at_least(at_most(max_chunks, at_most(at_least(16384 / nh, 8), kMaxSplits)), 1);
+  // (four heads per workgroup: a quarter of the segments, so four times as many pieces of each)
+  const int pieces = s.span > 1 ? at_most(at_least(32768 / nh, 8), kMaxSplits + 1) : at_most(at_least(16384 / nh, 8), kMaxSplits);
+  s.own.slots = s.whole ? 1 : at_least(at_most(s.span * max_chunks, pieces), 1);
   if (!any_shared) return s;
   const long cols = (long)(shared.max_group_seqs < c.n_seqs ? shared.max_group_seqs : c.n_seqs) * c.group;
   s.cols = cols <= 128 ? 128 : 256;
@@ -421,10 +446,10 @@ Split split_of(const PagedView &c, const SharedView &shared) {
 template <bool kShared>
 void launch_own(const PagedArgs &p, hipStream_t stream) {
   const dim3 grid(p.whole ? p.c.n_seqs * p.c.n_kv_heads : p.own.grid);
-  if (p.c.page_shift < 4)
-    hipLaunchKernelGGL((paged_kernel<true, kShared>), grid, dim3(kPagedThreads), 0, stream, p);
-  else
-    hipLaunchKernelGGL((paged_kernel<false, kShared>), grid, dim3(kPagedThreads), 0, stream, p);
+  const bool small = p.c.page_shift < 4;
+  const auto kernel = p.span > 1 ? small ? paged_kernel<true, kShared, kPagedWaves> : paged_kernel<false, kShared, kPagedWaves>
+                                 : small ? paged_kernel<true, kShared, 1> : paged_kernel<false, kShared, 1>;
+  hipLaunchKernelGGL(kernel, grid, dim3(kPagedThreads), 0, stream, p);
 }
 
 template <bool kShared>
@@ -432,7 +457,7 @@ void launch_merge(const PagedArgs &p, hipStream_t stream) {
   const int nh = p.c.n_seqs * p.c.n_q_heads;
   if (p.parts.all <= 32)
     hipLaunchKernelGGL((paged_merge_kernel<128, kShared>), dim3(nh), dim3(128), 0, stream, p);
-  else if (p.parts.all <= 64 || nh >= 512)
+  else if (p.parts.all <= 64 || nh >= 256)
     hipLaunchKernelGGL((paged_merge_kernel<256, kShared>), dim3(nh), dim3(256), 0, stream, p);
   else
     hipLaunchKernelGGL((paged_merge_kernel<1024, kShared>), dim3(nh), dim3(1024), 0, stream, p);
@@ -459,6 +484,7 @@ hipError_t launch_paged_decode(const PagedView &c, const PagedAttention &a, floa
   p.parts.ml = reinterpret_cast<float2 *>(partials + (size_t)c.n_seqs * c.n_q_heads * p.parts.all * kHeadDim);
   p.parts.pieces = reinterpret_cast<int32_t *>(p.parts.ml + (size_t)c.n_seqs * c.n_q_heads * p.parts.all);
   p.whole = s.whole;
+  p.span = s.span;
   p.own = s.own;
   p.shared = s.shared;
   p.shared_cols = s.cols;

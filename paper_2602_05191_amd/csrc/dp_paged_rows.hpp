@@ -151,6 +151,7 @@ struct PagedArgs {
   Partials parts;
   int32_t head0;        // this launch serves heads [head0, head0 + 16) of every group
   int32_t whole;        // own rows: nothing dealt out, a workgroup per segment (which writes the output where none are shared)
+  int32_t span;         // own rows: KV heads per workgroup, 1 or 4
   Deal own, shared;     // shared.slots == 0: no shared rows
   int32_t shared_cols;  // columns (sequences x query heads of a KV head) per workgroup over shared rows
   float scale_log2;
@@ -160,13 +161,13 @@ struct PagedArgs {
 // what is subtracted from a score whose running maximum is m
 __device__ __forceinline__ float finite_max(float m) { return fmaxf(m, -3.402823466e38f); }
 
-// Rows [first, len) of a sequence; its chunks are [first / 64, ceil(len / 64)).
+// Own rows are dealt out in chunks of 64 rows of one KV head, or of 16 of four (span).
+__host__ __device__ constexpr int own_chunk(int span) { return kChunkRows / span; }
+
+// Rows [first, len) of a sequence; in chunks of n rows they are [first / n, ceil(len / n)).
 struct SeqRows {
   int first, len;
-  __device__ __forceinline__ int chunk0() const { return first / kChunkRows; }
-  __device__ __forceinline__ int chunks() const {
-    return first < len ? (len + kChunkRows - 1) / kChunkRows - chunk0() : 0;
-  }
+  __device__ __forceinline__ int chunks(int n) const { return first < len ? (len + n - 1) / n - first / n : 0; }
 };
 template <bool kShared>
 __device__ __forceinline__ SeqRows seq_rows(const PagedArgs &p, int s) {
@@ -179,12 +180,12 @@ __device__ __forceinline__ SeqRows seq_rows(const PagedArgs &p, int s) {
     r.first = p.a.first_rows ? max(0, p.a.first_rows[s]) : 0;
   return r;
 }
-// sequences, and the KV heads of each
-template <bool kShared>
+// sequences, and the KV heads (or groups of them) of each
+template <bool kShared, int kSpan>
 __device__ __forceinline__ auto own_segments(const PagedArgs &p) {
   return [&p](int s) {
     const SeqRows r = seq_rows<kShared>(p, s);
-    return Segments{r.chunks(), p.c.n_kv_heads, r.first, r.len};
+    return Segments{r.chunks(own_chunk(kSpan)), p.c.n_kv_heads / kSpan, r.first, r.len};
   };
 }
 

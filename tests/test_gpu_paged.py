@@ -411,6 +411,42 @@ def test_decode_of_very_many_sequences(dp, layout):
     P.check(paged(dp, pool, q, layout), P.decode(pool, q))
 
 
+def wide_bound(n_seqs, n_kv, page):
+    """max_len from which on four KV heads that lie side by side are read by one workgroup, and the table's width for it."""
+    longest = -(-4096 // (n_seqs * n_kv)) * 64
+    return longest, -(-longest // page)
+
+
+@pytest.mark.parametrize("n_kv, group", [(4, 1), (8, 4), (4, 16), (4, 20), (12, 5)])
+@pytest.mark.parametrize("page", [1, 8, 16, 64, 256])
+def test_decode_of_heads_side_by_side(dp, n_kv, group, page):
+    """Tokens outermost and a bound of many rows: four KV heads per workgroup.  First rows inside a tile, behind the end and
+    negative, a prior for some heads, idle sequences, pages that are not there."""
+    lens = [700, 17, 0, 1, 333, 64, 2049]
+    first = [0, 16, 0, 0, 101, 64, -3]
+    longest, width = wide_bound(len(lens), n_kv, page)
+    longest = max(longest, 2049)
+    pool = P.Pool(lens, n_kv, page, seed=51 + page, extra=0, width=max(width, -(-2049 // page)))
+    pool.table[4, -(-150 // page)] = -7 if 150 + page < 333 else pool.table[4, -(-150 // page)]
+    q = queries(pool.rng, len(lens), n_kv * group)
+    prior = [pool.rng.standard_normal((len(lens), n_kv * group, 128)).astype(np.float32),
+             pool.rng.uniform(-5, 9, (len(lens), n_kv * group)).astype(np.float32)]
+    prior[1][1] = -np.inf
+    P.check(paged(dp, pool, q, "token", first=first, prior=prior, max_len=longest), P.decode(pool, q, first, prior))
+    got = paged(dp, pool, q, "token", max_len=longest)
+    P.check(got, P.decode(pool, q))
+    assert all(torch.equal(x, y) for x, y in zip(got, paged(dp, pool, q, "token", max_len=longest)))
+
+
+@pytest.mark.parametrize("lens", [[40000], [9000, 3, 0, 20000], [1100] * 40])
+def test_decode_of_heads_side_by_side_splits(dp, lens):
+    """The same with rows enough for every workgroup; a bound beyond the lengths."""
+    n_kv = 8 if len(lens) == 1 else 4
+    pool = P.Pool(lens, n_kv, 16, seed=len(lens), extra=0, width=4096)
+    q = queries(pool.rng, len(lens), 4 * n_kv, scale=1.5)
+    P.check(paged(dp, pool, q, "token", torch.bfloat16, max_len=65536), P.decode(pool, q), torch.bfloat16)
+
+
 @pytest.mark.parametrize("form", ["wide_table", "no_lse", "odd_out", "raw_bits"])
 def test_forms_of_arguments(dp, form):
     """A table that is a slice of a wider one; no lse; an output at an odd element; queries and pages as raw bits."""
@@ -606,6 +642,18 @@ def test_shared_prefix_keeps_what_is_not_finite_in_its_place(dp, dtype):
             pool.v[pool.table[0, 250 // 16], 0, 250 % 16, 5] = H_INF
             out, _ = shared_decode(dp, pool, q, [0, 9], [300], dtype=dtype)
             assert torch.isposinf(out[..., 5]).all() and torch.isfinite(out).sum() == out.numel() - 9 * 4
+
+
+@pytest.mark.parametrize("page", [4, 64])
+def test_shared_groups_of_heads_side_by_side(dp, page):
+    """Own rows of four KV heads per workgroup behind shared ones."""
+    ptr, shared = [1, 6, 8], [333, 1000]
+    pool = shared_pool(ptr, shared, [40, 200, 33, 0, 90, 7, 1500, 61, 300], 4, page, seed=52, idle=(3,))
+    longest, width = wide_bound(9, 4, page)
+    longest, width = max(longest + 1024, 2500), max(width + -(-1024 // page), -(-2500 // page))
+    pool.table = np.pad(pool.table, ((0, 0), (0, width - pool.table.shape[1])), constant_values=-1)
+    q = queries(pool.rng, 9, 20)
+    P.check(shared_decode(dp, pool, q, ptr, shared, layout="token", max_len=longest), P.decode(pool, q))
 
 
 @pytest.mark.parametrize("n_seqs", [9, 40])
