@@ -421,7 +421,8 @@ dp_status dp_append_kv(const dp_paged_cache *cache, const dp_kv_append *tokens, 
  *   out = (e^prior_lse prior_out + Z o) / (e^prior_lse + Z),  lse = ln(e^prior_lse + Z),
  * Z and o the normaliser and the output of the pages' rows.  prior_out may be out (of fp32), prior_lse may be lse.
  *   q          bf16 [n_seqs, n_q_heads, head_dim], 16-byte aligned
- *   out, lse   as dp_sparse_decode; no row and no prior (prior_lse = -inf): out = 0, lse = -inf
+ *   out, lse   as dp_sparse_decode; no row and no prior (prior_lse = -inf), rows that all score -inf as well: out = 0,
+ *              lse = -inf.  A score of NaN or +inf among the rows, or such a prior_lse: NaN, both.
  * Rows behind a sequence's last token (the rest of its last page) may hold anything, NaN included.
  * workspace: dp_paged_workspace_bytes (0 for an invalid cache), 256-byte aligned. */
 size_t dp_paged_workspace_bytes(const dp_paged_cache *cache);

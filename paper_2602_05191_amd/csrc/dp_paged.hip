@@ -131,9 +131,11 @@ __device__ __forceinline__ void store_head(const PagedArgs &p, int64_t head, int
   const float L = fmaf(x.l, w, wp);
   float o = x.m > -INFINITY ? x.o * w : 0.f;
   if (prior > -INFINITY) o = fmaf(prior_o, wp, o);  // (a prior without weight may hold anything)
-  const bool any = L > 0.f;
-  store_out(p.attn.out, p.attn.out_is_bf16, head, d, any ? o / L : 0.f);
-  if (p.attn.lse && d == 0) p.attn.lse[head] = any ? fmaf(log2f(L), kLn2, M) : -INFINITY;
+  // Nothing attended: a sum of exactly zero, for a row whose score is subtracted, or the prior, has a weight of one.  A score
+  // or a prior of NaN or +inf leaves a sum of NaN, and that is the result.
+  const bool none = L == 0.f;
+  store_out(p.attn.out, p.attn.out_is_bf16, head, d, none ? 0.f : o / L);
+  if (p.attn.lse && d == 0) p.attn.lse[head] = none ? -INFINITY : fmaf(log2f(L), kLn2, M);
 }
 
 template <bool kSmallPages, bool kShared, int kSpan>
