@@ -7,13 +7,12 @@
 //   output  O^T[dims x heads] += V^T P^T, v_mfma_f32_16x16x16_bf16, k = 4 (l / 16) + i: the weights are where the scores
 //           were, and of the values a lane loads dims 8 (l % 16) .. + 7 of its four rows and puts the rows of a dimension
 //           side by side by byte permutes.  Tile n of eight holds dims 8 x + n.
-// A weight goes into the product as three bf16 numbers that add up to its 24 bits; the sum of the weights is taken from the
-// fp32 weights.  The first two are cut, not rounded, and what is left is increased by 2^-26 and 2^-34 of the weight: none is
-// zero, so that an infinite value does not become NaN (0 x inf).
+// A weight goes into the product as three bf16 numbers that add up to its 24 bits, the first two cut, not rounded, none of
+// them zero (an infinite value would become NaN).  The sum of the weights is taken from the fp32 weights.
 // What is subtracted from a head's scores is a score that was its largest at some time, unscaled (the largest weight is in
 // order whatever the size of the scores); it moves when one leads it by 8 in base 2: weights up to 2^8 lose nothing in fp32.
 // A maximum of -inf is taken as the lowest finite number when it is subtracted.  A weight below 2^-126 of the largest counts
-// as zero (v_exp_f32).
+// as zero (v_exp_f32), also times an infinite value.
 // Tiles begin at multiples of 16 rows, so a tile of pages of 16 tokens or more lies in one page: its place is a scalar and
 // a lane's offsets are the same for every tile.  The numbers of the pages of a wave's next 64 tiles are fetched by its 64
 // lanes at once.  Smaller pages: every row's page by the lane that loads the row's key, a tile ahead of the rows.
@@ -38,6 +37,7 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPagedThreads = 256;
@@ -216,12 +216,13 @@ __global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(2
         float rest = w;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-          const float cut = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
           piece[q][i] = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(rest) >> 16));
-          rest = fmaf(w, q == 0 ? 0x1p-26f : 0x1p-34f, rest - cut);
+          rest -= __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
         }
         piece[2][i] = (__bf16)rest;
       }
+#pragma unroll
+      for (int q = 1; q < 3; ++q) piece[q] = not_zero<u16x4>(piece[q], piece[0]);
       l += (x[0] + x[1]) + (x[2] + x[3]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {  // dims 2 j, 2 j + 1 of the lane's eight: the four rows' values side by side

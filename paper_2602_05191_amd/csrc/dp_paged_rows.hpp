@@ -161,6 +161,16 @@ struct PagedArgs {
 // what is subtracted from a score whose running maximum is m
 __device__ __forceinline__ float finite_max(float m) { return fmaxf(m, -3.402823466e38f); }
 
+// Weights go into the products as bf16 pieces that add up.  A piece that ends up as zero although its weight is not becomes the
+// weight's exponent, read as a bf16 pattern: at most 2^-125, for the least weights 2^-133 (the matrix cores take numbers below
+// 2^-126 as they are).  An infinite value times a piece of zero would be NaN.  Patterns of numbers that are not negative are in
+// the numbers' order.  (64 sequences behind 32768 rows 110.8 us, 110.0 without; with the lesser of the pattern and 1 114.3.)
+template <class Bits, class Piece>
+__device__ __forceinline__ Piece not_zero(Piece piece, Piece first) {
+  return __builtin_bit_cast(Piece, __builtin_elementwise_max(__builtin_bit_cast(Bits, piece),
+                                                             __builtin_bit_cast(Bits, first) >> (Bits)7));
+}
+
 // Own rows are dealt out in chunks of 64 rows of one KV head, or of 16 of four (span).
 __host__ __device__ constexpr int own_chunk(int span) { return kChunkRows / span; }
 

@@ -10,9 +10,8 @@
 //           8 .. 11}.  Nothing moves between lanes but the two halves' maxima.
 // Weights go into the product in bf16 pieces that add up: two (16 bits) for a bf16 output, three (all 24) for fp32; their
 // sum is taken from the fp32 weights.  (One piece rounds a weight by up to 2^-9, as much as the output itself is rounded.)
-// All but the last piece are cut, not rounded, and what is left is increased by 2^-23 (three pieces: 2^-26, 2^-34) of the
-// weight: no piece is zero, so that an infinite value does not become NaN (0 x inf).
-// A weight below 2^-126 of the largest counts as zero here (v_exp_f32).
+// All but the last piece are cut, not rounded, and none is zero (an infinite value would become NaN).
+// A weight below 2^-126 of the largest counts as zero here (v_exp_f32), also times an infinite value.
 // What is subtracted from a column's scores is a score that was its largest at some time; it moves when one leads it by 8 in
 // base 2 (weights up to 2^8 lose nothing in fp32 or in pieces).  Moving with every new maximum, some of a wave's columns
 // had one in most tiles.
@@ -35,6 +34,7 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) s16x4 *LdsTile;
 
@@ -196,13 +196,13 @@ __global__ __launch_bounds__(kSharedThreads) __attribute__((amdgpu_waves_per_eu(
           float rest = x[8 * n + e];
 #pragma unroll
           for (int q = 0; q + 1 < kPieces; ++q) {
-            const float cut = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
             piece[q][e] = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(rest) >> 16));
-            rest = kPieces == 2 ? fmaf(rest, 1.f + 0x1p-23f, -cut)
-                                : fmaf(x[8 * n + e], q == 0 ? 0x1p-26f : 0x1p-34f, rest - cut);
+            rest -= __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
           }
           piece[kPieces - 1][e] = (__bf16)rest;
         }
+#pragma unroll
+        for (int q = 1; q < kPieces; ++q) piece[q] = not_zero<u16x8>(piece[q], piece[0]);
         bf16x8 value[4];
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) {

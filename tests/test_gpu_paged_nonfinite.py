@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paged as P
-from test_gpu_paged import Buffers, freqs_of, paged, q_dev, queries, shared_decode, shared_pool, wide_bound
+from test_gpu_paged import Buffers, freqs_of, only_dim_7, paged, q_dev, queries, shared_decode, shared_pool, wide_bound
 
 pytestmark = pytest.mark.gpu
 
@@ -52,6 +52,11 @@ def rows_of(pool, s, r, kv):
     return pool.table[s, r // pool.page], kv, r % pool.page
 
 
+def holders(pool, s, r):
+    """The sequences that attend row r of sequence s (on a page that they share, or alone)."""
+    return [t for t in range(len(pool.lens)) if pool.lens[t] > r and pool.table[t, r // pool.page] == pool.table[s, r // pool.page]]
+
+
 def check_heads(got, ref, bad, dtype):
     """The heads of bad are NaN, output and lse; the others are the reference's."""
     out, lse = got
@@ -77,11 +82,10 @@ def test_a_nan_query_or_key(dp, form, group, dtype):
     check_heads(run(odd, dtype), ref, bad, dtype)
     for s, r, kv in ((0, 0, 0), (0, 299, 1), (1, 30, 1)):
         at = rows_of(pool, s, r, kv)
-        sharers = {t for t in range(len(pool.lens)) if pool.lens[t] > r and pool.table[t, r // pool.page] == at[0]}
         keep = pool.k[at].copy()
         pool.k[at][7] = NAN
         bad = np.zeros(q.shape[:2], dtype=bool)
-        for t in sharers:
+        for t in holders(pool, s, r):
             bad[t, kv * group:(kv + 1) * group] = True
         check_heads(run(q, dtype), ref, bad, dtype)
         pool.k[at] = keep
@@ -96,11 +100,10 @@ def test_an_infinite_key(dp, form, dtype):
     q[:, 0::2, 7], q[:, 1::2, 7] = ONE, MINUS_ONE
     for s, r in ((0, 0), (0, 150), (1, 36), (0, 299)):
         at = rows_of(pool, s, r, 1)
-        sharers = {t for t in range(len(pool.lens)) if pool.lens[t] > r and pool.table[t, r // pool.page] == at[0]}
         keep = pool.k[at].copy()
         pool.k[at][7] = INF
         bad = np.zeros(q.shape[:2], dtype=bool)
-        for t in sharers:
+        for t in holders(pool, s, r):
             bad[t, 4:8:2] = True
         check_heads(run(q, dtype), P.decode(pool, q), bad, dtype)
         pool.k[at] = keep
@@ -142,3 +145,38 @@ def test_a_nan_key_is_appended_and_attended(dp):
     bad[0, 4:] = True
     assert torch.isnan(out[bad]).all() and torch.isnan(lse[bad]).all()
     assert torch.isfinite(out[~bad]).all() and torch.isfinite(lse[~bad]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("lead", [60.0, 99.0, 100.0, 110.0, 118.0, 125.0, 125.5])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_an_infinite_value_of_little_weight(dp, form, lead, dtype):
+    """One row leads all others by 60 to 125.5 in base 2 (a weight that is a power of two leaves nothing of itself for a second
+    piece); an infinite value in front of it, next to it and far behind it stays in its dimension: +inf there, in all heads
+    that attend the row, nothing elsewhere."""
+    pool, q, run = make(dp, form)
+    leader, scale = int(pool.lens[0]) // 2, float(np.float32(np.log(2)))   # (times log2 e: 1 in fp32)
+    only_dim_7(pool, q, lambda i: np.where(i == leader, lead, 0.0))
+    ref = P.decode(pool, q, scale=scale)
+    for r in (0, leader + 1, int(pool.lens[0]) - 1):
+        at = rows_of(pool, 0, r, 1)
+        keep = pool.v[at].copy()
+        pool.v[at][5] = INF
+        out, lse = run(q, dtype, sm_scale=scale)
+        for t in holders(pool, 0, r):
+            assert torch.isposinf(out[t, 4:8, 5]).all()
+            out[t, 4:8, 5] = torch.from_numpy(ref[0][t, 4:8, 5]).to(out)
+        P.check((out, lse), ref, dtype)
+        pool.v[at] = keep
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_large_values_without_weight(dp, form, dtype):
+    """Rows that score -inf hold the largest numbers there are: no trace of them."""
+    pool, q, run = make(dp, form)
+    q[..., 7] = ONE
+    for r in (0, 33, 150, 299):
+        at = rows_of(pool, 0, r, 1)
+        pool.k[at][7], pool.v[at] = NINF, 0x7F7F
+    P.check(run(q, dtype), P.decode(pool, q), dtype)
