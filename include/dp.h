@@ -389,7 +389,8 @@ typedef struct {
  * [0, max_seq_len) or on a page that is not there is rotated (q_out) and not stored.
  *   q, k, v   [n_tokens, heads, head_dim] of dtype, a token every q_stride (k_stride, v_stride) elements, its heads next
  *             to each other: slices of one projection's output.  16-byte aligned, strides multiples of 16 bytes.
- *   q_out     bf16 [n_tokens, n_q_heads, head_dim]; may be q itself where that is bf16 and contiguous
+ *   q_out     bf16 [n_tokens, n_q_heads, head_dim]; may be q itself where that is bf16 and contiguous.  Otherwise over no row
+ *             of q, k or v (DP_ERR_INVALID_ARG): it is written while they are read
  * Rotation of k and q to the token's position p (positions[token], or its place in the sequence): the first rope_dims
  * dimensions form pairs i, dimensions (i, i + rope_dims/2), with DP_ROPE_ADJACENT_PAIRS (2i, 2i + 1), and
  *   (a, b) -> (a cos t - b sin t, a sin t + b cos t),   t = p * rope_freqs[i]

@@ -274,6 +274,17 @@ constexpr int32_t kMaxAppendTokens = 1 << 25;  // (the same)
 
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
+// Whether one of n rows of row_bytes, one every stride bytes, has a byte in [to, to + to_bytes).
+bool rows_touch(const void *rows, int64_t n, int64_t stride, int64_t row_bytes, const void *to, int64_t to_bytes) {
+  const int64_t ahead = (int64_t)(reinterpret_cast<uintptr_t>(to) - reinterpret_cast<uintptr_t>(rows));
+  int64_t i = 0;  // the first row that ends behind `to`
+  if (ahead >= row_bytes) {
+    if (stride == 0) return false;
+    i = (ahead - row_bytes) / stride + 1;
+  }
+  return i < n && i * stride < ahead + to_bytes;
+}
+
 dp_status paged_ok(const dp_paged_cache *c) {
   if (!c || c->n_seqs <= 0 || c->n_kv_heads <= 0 || c->n_q_heads <= 0 || c->n_q_heads % c->n_kv_heads ||
       c->n_pages < 0 || c->page_size <= 0 || c->page_stride < 0 || c->head_stride < 0 || c->slot_stride < 0 ||
@@ -717,6 +728,17 @@ dp_status dp_append_kv(const dp_paged_cache *cache, const dp_kv_append *tokens, 
     if (stride < 0 || stride * size % 16 || stride > ((int64_t)1 << 58) / tokens->n_tokens) return DP_ERR_INVALID_ARG;
   if (!aligned16(tokens->k) || !aligned16(tokens->v) || (tokens->q && (!aligned16(tokens->q) || !aligned16(tokens->q_out))))
     return DP_ERR_INVALID_ARG;
+  // q_out is written while other tokens' rows are read: over none of them, but a row of q over itself
+  if (tokens->q) {
+    const int64_t n = tokens->n_tokens, row = (int64_t)dp::kHeadDim * size;
+    const int64_t q_row = cache->n_q_heads * row, kv_row = cache->n_kv_heads * row;
+    const int64_t out_row = cache->n_q_heads * (int64_t)dp::kHeadDim * 2;
+    const bool in_place = tokens->q_out == tokens->q && size == 2 && (n == 1 || tokens->q_stride * size == out_row);
+    if ((!in_place && rows_touch(tokens->q, n, tokens->q_stride * size, q_row, tokens->q_out, n * out_row)) ||
+        rows_touch(tokens->k, n, tokens->k_stride * size, kv_row, tokens->q_out, n * out_row) ||
+        rows_touch(tokens->v, n, tokens->v_stride * size, kv_row, tokens->q_out, n * out_row))
+      return DP_ERR_INVALID_ARG;
+  }
   dp::AppendTokens t;
   t.n_tokens = tokens->n_tokens;
   t.is_f32 = tokens->dtype == DP_F32;

@@ -198,6 +198,29 @@ def test_append_keys_and_values_only_and_queries_in_place(dp):
     assert np.array_equal(P.bits(other), P.bits(qd)) and P.turned_close(P.bits(qd), given, [32, 1, 6], f, False)
 
 
+def test_append_writes_queries_between_what_it_reads(dp):
+    """q_out in the gap between two tokens' rows of q, k and v; one strided token in place; neither touches a row that is read."""
+    pool = P.Pool([9, 5], 2, 16, seed=46)
+    c, f = pool.device(6), torch.tensor(freqs_of(128), device="cuda")
+    x = torch.from_numpy(pool.rng.standard_normal((2, 40, 128))).to(torch.bfloat16).cuda()
+    q, k, v, gap = x[:, :6], x[:, 6:8], x[:, 8:10], x[0, 20:32].view(2, 6, 128)
+    want, given = torch.empty(2, 6, 128, dtype=torch.bfloat16, device="cuda"), x.clone()
+    dp.dp_append_kv(c, k, v, f, q=q, q_out=want)
+    stored = c.k_pages.clone(), c.v_pages.clone()
+    dp.dp_append_kv(c, k, v, f, q=q, q_out=gap)
+    torch.cuda.synchronize()
+    assert torch.equal(gap, want) and torch.equal(c.k_pages, stored[0]) and torch.equal(c.v_pages, stored[1])
+    given[0, 20:32] = want.view(12, 128)
+    assert torch.equal(x, given)
+    one = P.Pool([9], 2, 16, seed=47).device(6)
+    dp.dp_append_kv(one, k[:1], v[:1], f, q=q[:1], q_out=q[:1])
+    torch.cuda.synchronize()
+    given[0, :6] = want[0]
+    assert torch.equal(x, given)
+    with pytest.raises(dp.DPError):
+        dp.dp_append_kv(c, k, v, f, q=x[:, 28:34], q_out=gap)   # (the first token's heads of this q lie in the gap)
+
+
 def test_append_of_many_tokens_is_the_append_of_its_parts(dp):
     """A prompt beyond 256 MiB of rows (written past the caches) and the same one in three parts (which are not): same bits."""
     n, n_kv, n_q, page = 120000, 2, 6, 64

@@ -178,3 +178,24 @@ def test_the_reference_turns_pairs():
     f = [np.pi / 2] + [0.0] * 15
     assert np.abs(P.rotate(x, [1], f, True)[0, 0, 1] - 1) < 1e-15 and np.abs(P.rotate(x, [1], f, False)[0, 0, 16] - 1) < 1e-15
     assert np.abs(P.rotate(x, [2], f, True)[0, 0, 0] + 1) < 1e-15
+
+
+ROWS = 4 * 8 * 128   # elements of q_out: 4 tokens of 8 heads
+FAR = 1 << 30
+
+
+@pytest.mark.parametrize("bad", [
+    dict(dtype=1),                                                    # fp32 queries in place: rows of q_out lie on other tokens'
+    dict(q_stride=1536), dict(q_stride=0),                            # in place, not contiguous
+    dict(q=FAR + 16), dict(q=FAR - 16), dict(q=FAR + 2 * ROWS - 16), dict(q=FAR - 2 * ROWS + 16),
+    dict(q=FAR - 3 * 2 * 1536, q_stride=1536),                        # the last token's row is q_out's first
+    dict(q=FAR - 2 * 2 * 99328 - 2 * 1008, q_stride=99328),           # one token's last 16 numbers reach it, q_out lies in a gap else
+    dict(q=FAR + 2 * ROWS - 2 * 8, q_stride=99328),
+    dict(k=FAR), dict(v=FAR), dict(k=FAR + 2 * ROWS - 16), dict(v=FAR - 3 * 512 - 512 + 16),
+    dict(k=FAR - 2 * 2048, k_stride=1024), dict(v=FAR + 4096, v_stride=0),
+    dict(n_tokens=1, tok_ptr=ONE, dtype=1),
+])
+def test_rotated_queries_that_would_overwrite_what_is_read(lib, bad):
+    kw = dict(q=FAR, q_out=FAR, k=2 * FAR, v=3 * FAR)
+    kw.update(bad)
+    assert lib.dp_append_kv(C.byref(cache()), C.byref(append(**kw)), None) == INVALID
