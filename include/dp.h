@@ -368,8 +368,9 @@ dp_status dp_kmeans_fit(const dp_prefill *in, void *centroids, int32_t n_iters, 
  *   page_table  an entry outside [0, n_pages) is a page that is not there: nothing is written to it, and its tokens
  *               are left out of attention.  Entries behind the last token of a sequence are not read.
  * Two sequences may share pages (dp_shared_prefix_decode).
- * DP_ERR_UNSUPPORTED: head_dim != 128, a page_size that is no power of two, more than 2^22 sequences x query heads or 2^30
- * rows of a sequence, strides that pass 2^30 elements inside a page. */
+ * DP_ERR_UNSUPPORTED: head_dim != 128, a page_size that is no power of two, more than 2^22 sequences x query heads, 2^30 rows
+ * of a sequence or (by max_seq_len) 2^31 - 512 chunks of 64 rows of all query heads, strides that pass 2^30 elements inside a
+ * page. */
 typedef struct {
   int32_t n_seqs, n_kv_heads, n_q_heads, head_dim; /* n_q_heads % n_kv_heads == 0; head_dim == 128        */
   int32_t n_pages, page_size;                      /* page_size a power of two                            */

@@ -269,6 +269,8 @@ dp_status static_scratch(void **ptr) {
 // ---- paged cache ----
 constexpr int64_t kMaxPagedHeads = 1 << 22;  // sequences x query heads of a call (grid sizes stay below 2^32 threads)
 constexpr int32_t kMaxPagedLen = 1 << 30;    // rows of a sequence (a row number plus a round of tiles stays below 2^31)
+// chunks of rows of a call, which the kernels number in 32 bits, shares of up to 512 workgroups of them included
+constexpr int64_t kMaxPagedChunks = ((int64_t)1 << 31) - 512;
 
 constexpr int32_t kMaxAppendTokens = 1 << 25;  // (the same)
 
@@ -295,7 +297,7 @@ dp_status paged_ok(const dp_paged_cache *c) {
     return DP_ERR_INVALID_ARG;
   if (c->head_dim != dp::kHeadDim || (c->page_size & (c->page_size - 1)) ||
       (int64_t)c->n_seqs * c->n_q_heads > kMaxPagedHeads || c->max_seq_len > kMaxPagedLen ||
-      (int64_t)c->n_seqs * c->n_q_heads * (c->max_seq_len / dp::kChunkRows + 1) >= (int64_t)1 << 31)
+      (int64_t)c->n_seqs * c->n_q_heads * (c->max_seq_len / dp::kChunkRows + 1) >= kMaxPagedChunks)
     return DP_ERR_UNSUPPORTED;
   // the places of a pool fit 64 bits, those of a head's rows inside a page 31
   constexpr int64_t kMost = (int64_t)1 << 58;

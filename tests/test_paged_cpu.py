@@ -199,3 +199,21 @@ def test_rotated_queries_that_would_overwrite_what_is_read(lib, bad):
     kw = dict(q=FAR, q_out=FAR, k=2 * FAR, v=3 * FAR)
     kw.update(bad)
     assert lib.dp_append_kv(C.byref(cache()), C.byref(append(**kw)), None) == INVALID
+
+
+@pytest.mark.parametrize("heads, rows", [(200, 64 * 10737417), (256, 64 * ((1 << 23) - 3) + 1), (128, 64 * ((1 << 24) - 5)), (510, 64 * 4210751)])
+def test_rows_are_counted_in_32_bits(lib, heads, rows):
+    """A call's chunks of 64 rows, and one round of shares of them that 512 workgroups take, stay below 2^31: what passes it
+    is refused, what is just below is not."""
+    def room(rows):
+        c = cache(n_seqs=1, n_kv_heads=heads, n_q_heads=heads, page_size=1 << 14, page_stride=0, head_stride=0, slot_stride=8,
+                  max_seq_len=rows, table_stride=1 << 17)
+        return lib.dp_paged_workspace_bytes(C.byref(c))
+    while True:
+        chunks = heads * -(-rows // 64)
+        share = -(-chunks // 512)
+        if 512 * share < 1 << 31 and chunks + 511 < 1 << 31:
+            break
+        assert room(rows) == 0
+        rows -= 64
+    assert room(rows - 2 * 64) > 0
