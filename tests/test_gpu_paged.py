@@ -244,6 +244,35 @@ def test_append_of_many_tokens_is_the_append_of_its_parts(dp):
     assert P.turned_close(P.bits(results[0][1][at]), P.wide(q[at]), at, freqs_of(128), False)
 
 
+def test_append_of_many_fp32_tokens_is_the_append_of_its_parts(dp):
+    """The same from fp32, pairs side by side, into pages with the tokens outermost, keys and values in strides of their own."""
+    n, n_kv, n_q, page = 130000, 4, 4, 16
+    gen = torch.Generator("cuda").manual_seed(3)
+    x = torch.randn(n, n_q + n_kv + 1, 128, device="cuda", generator=gen)
+    v = torch.randn(n, n_kv, 128, device="cuda", generator=gen)
+    q, k = x[:, :n_q], x[:, n_q:n_q + n_kv]
+    f = torch.tensor(freqs_of(96), device="cuda")
+    table = torch.randperm(n // page, generator=torch.Generator().manual_seed(4)).int().cuda()[None]
+    results = []
+    for cuts in ([0, n], [0, 60000, 60007, n]):
+        pages = torch.zeros(2, n // page, page, n_kv, 128, device="cuda", dtype=torch.bfloat16)
+        lens = torch.zeros(1, device="cuda", dtype=torch.int32)
+        c = dp.PagedCache(pages[0].transpose(1, 2), pages[1].transpose(1, 2), table, lens, n, n_q)
+        out = torch.empty(n, n_q, 128, device="cuda", dtype=torch.bfloat16)
+        for a, b in zip(cuts, cuts[1:]):
+            lens.fill_(b)
+            dp.dp_append_kv(c, k[a:b], v[a:b], f, q=q[a:b], q_out=out[a:b], tok_ptr=up([0, b - a]), adjacent_pairs=True)
+        results.append((pages, out))
+    torch.cuda.synchronize()
+    assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
+    at = [0, 88888, n - 1]
+    assert P.turned_close(P.bits(results[0][1][at]), P.wide(q[at]), at, freqs_of(96), True)
+    places = table[0, [i // page for i in at]].long().cpu().tolist()
+    for i, p in zip(at, places):
+        assert P.turned_close(P.bits(results[0][0][0, p, i % page][None]), P.wide(k[i:i + 1]), [i], freqs_of(96), True)
+        assert torch.equal(results[0][0][1, p, i % page], v[i].to(torch.bfloat16))
+
+
 def test_append_keeps_infinities_and_nan_in_their_pair(dp):
     lens, f = [5], freqs_of(64)
     for bad, dims in ((np.inf, (3, 35)), (np.nan, (3, 35)), (np.inf, (100,))):
