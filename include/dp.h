@@ -364,7 +364,8 @@ dp_status dp_kmeans_fit(const dp_prefill *in, void *centroids, int32_t n_iters, 
  * sequence s lies in slot i % page_size of page page_table[s * table_stride + i / page_size]; its row of KV head h starts
  * at element page * page_stride + h * head_stride + slot * slot_stride of k_pages and v_pages (so a pool may keep the
  * heads or the tokens of a page outermost, or K and V of a page side by side).
- *   seq_lens    tokens of each sequence; larger values than max_seq_len are clamped to it, negative ones to 0
+ *   seq_lens    tokens of each sequence; attention clamps larger values than max_seq_len to it, negative ones to 0 (what
+ *               dp_append_kv is to store there has no place)
  *   page_table  an entry outside [0, n_pages) is a page that is not there: nothing is written to it, and its tokens
  *               are left out of attention.  Entries behind the last token of a sequence are not read.
  * Two sequences may share pages (dp_shared_prefix_decode).
@@ -412,12 +413,14 @@ typedef struct {
 } dp_kv_append;
 
 /* Stores the new tokens' keys (rotated) and values in the pages of the cache and the rotated queries in q_out.  Nothing
- * else of the pool is written.  Two tokens with the same place, or two sequences that append to one page's slot, leave
- * one of the two there.  Bitwise reproducible.  n_tokens == 0 does nothing; DP_ERR_UNSUPPORTED above 2^25. */
+ * else of the pool is written.  Bitwise reproducible where no two tokens have the same place.  Where they do (also two
+ * sequences that append to one page's slot) every row of the place, a KV head's key or its value, is one of theirs, each for
+ * itself and not the same one in every run.  n_tokens == 0 does nothing; DP_ERR_UNSUPPORTED above 2^25. */
 dp_status dp_append_kv(const dp_paged_cache *cache, const dp_kv_append *tokens, void *stream);
 
 /* Dense attention (Sec. 2.1, Eq. 1) of one query token per sequence over rows [first_rows[s], seq_lens[s]) of its pages
- * (first_rows NULL: from 0; negative values count as 0), for all query heads of a GQA group at once (any group size).
+ * (first_rows NULL: from 0; negative values count as 0), for all query heads of a GQA group at once (any group size;
+ * the rows are read once per 16 of them).
  * What a step over the clustered prompt left (out and lse of dp_decode_attention in fp32) is joined where prior_out and
  * prior_lse are given (both or neither): the result is attention over both parts,
  *   out = (e^prior_lse prior_out + Z o) / (e^prior_lse + Z),  lse = ln(e^prior_lse + Z),
@@ -449,7 +452,8 @@ typedef struct {
 /* dp_paged_decode (all rows, no prior) with the shared rows of a group read once for all its sequences, through the
  * table of its first sequence that is long enough to hold them.  Where that would take longer (few sequences, few shared
  * rows: the host decides by the bounds) every sequence is attended for itself, through its own table, unless
- * DP_SHARED_PREFIX_ONCE is set; so it is with more than 4096 groups. */
+ * DP_SHARED_PREFIX_ONCE is set; so it is with more than 4096 groups.  Of the weights of rows that are read once 16 bits enter a
+ * bf16 output (whose own rounding is 9 bits), all 24 an fp32 output and every lse. */
 #define DP_SHARED_PREFIX_ONCE 1u
 size_t dp_shared_prefix_workspace_bytes(const dp_paged_cache *cache, const dp_shared_prefix *prefix);
 dp_status dp_shared_prefix_decode(const dp_paged_cache *cache, const dp_shared_prefix *prefix, const void *q, void *out,

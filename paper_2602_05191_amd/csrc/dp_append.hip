@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView c, App
 
 hipError_t launch_append(const PagedView &c, const AppendTokens &t, hipStream_t s) {
   // A token's rows by one wave where there are enough tokens to fill the chip, else by several, down to four rows each: a
-  // call is then one round of loads.  us: one token of 48 rows 7.6 with one wave, 3.3 with twelve; 64 tokens 8.7 / 4.4.
+  // call is then one round of loads.  us: one token of 48 rows 7.6 with one wave, 3.7 with twelve; 64 tokens 8.7 / 4.2.
   constexpr int kChipWaves = 8192;
   const int rows = 2 * c.n_kv_heads + (t.q ? c.n_q_heads : 0), most = (rows + 3) / 4, want = kChipWaves / t.n_tokens;
   const int parts = want < 1 ? 1 : want < most ? want : most;

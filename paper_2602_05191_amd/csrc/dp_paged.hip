@@ -15,17 +15,19 @@
 // as zero (v_exp_f32), also times an infinite value.
 // Tiles begin at multiples of 16 rows, so a tile of pages of 16 tokens or more lies in one page: its place is a scalar and
 // a lane's offsets are the same for every tile.  The numbers of the pages of a wave's next 64 tiles are fetched by its 64
-// lanes at once.  Smaller pages: every row's page by the lane that loads the row's key, a tile ahead of the rows.
+// lanes at once.  Smaller pages: every row's page by the lane that loads the row's key, a tile ahead of the rows (16 sequences
+// of up to 65536 rows, pages of 1, 2, 4, 8 tokens 435, 451, 426, 422 us per call, of 16 and 64 412 and 403; tokens outermost
+// 435, 425, 419, 416, 410, 410).
 // A tile has a mask of 16 rows (inside [first, len) and on a page that is there); rows without a bit score -inf and their
 // values are made zero: they may hold anything.
 // Work split: the rows of all (sequence, KV head) segments, in chunks of 64, are dealt out evenly to one round of resident
 // workgroups; pieces are merged by a second kernel.  Short or very many segments are taken whole, a workgroup each, which
 // then writes the output itself.  Where the heads of a token lie side by side a workgroup's waves take the same rows of four
 // KV heads (chunks of 16 rows), not a head's rows in turn: what lies next to each other is read at one time.
-// Measured (8 KV heads, G = 4): 16 sequences of up to 65536 rows, 2.6 GB, 399 us = 6.5 TB/s, as much as this card reads (the
-// matrix cores are busy 16 % of it); one of 131072 rows 82.8 us (6.5 TB/s) and 6.2 for the merge; heads side by side, G = 8,
-// four of 131072 rows 332 us (6.5 TB/s; 372 with a head per workgroup).  Two tiles per wave in registers, one of them in
-// flight, two waves per SIMD; with a third tile the registers do not suffice (131072 rows: 97 us).
+// Measured (8 KV heads, G = 4): 16 sequences of up to 65536 rows, 2.6 GB, 399 us = 6.5 TB/s, 94 % of what the longest plain
+// stream reads here (the matrix cores are busy 16 % of it); one of 131072 rows 82.8 us (6.5 TB/s) and 6.9 for the merge;
+// heads side by side, G = 8, four of 131072 rows 332 us (6.5 TB/s; 372 with a head per workgroup).  Two tiles per wave in
+// registers, one of them in flight, two waves per SIMD; with a third tile the registers do not suffice (131072 rows: 97 us).
 #include "dp_attend.hpp"
 #include "dp_device.hpp"
 #include "dp_kernels.hpp"
@@ -412,6 +414,8 @@ Split split_of(const PagedView &c, const SharedView &shared) {
   // Whole segments against dealt-out chunks, us, G = 4, pages of 16 (segments of equal length): 8 segments of 512 rows 9.1 /
   // 10.0, of 768 11.3 / 9.9; 64 of 512 10.8 / 11.9, of 768 14.3 / 13.5; 128 of 768 15.7 / 15.7, of 1024 19.6 / 18.6; 256 of
   // 1536 33.4 / 38.1, ragged ones of up to 2048 36.0 / 34.2; 512 of 1024 43.2 / 48.0, ragged of up to 2048 67.6 / 63.6.
+  // (By the bound of the lengths.  One of 131072 instead of the longest: 1 x 1000 rows of one KV head 9.3 -> 10.7 us per call, of 8
+  // KV heads 1 x 4096 11.7 -> 13.7, 32 ragged of up to 700 14.9 -> 19.5, 64 x 512 23.3 -> 28.1, 16 x 4096 no change.)
   s.whole = c.n_seqs > kDealtItems || c.max_seq_len <= (n_seg >= 256 ? 1536 : n_seg >= 128 ? 768 : 640);
   // Shared rows are read once where that saves more than 48 MiB of reads and 4 MiB per sequence: below, the launches that it
   // takes cost more than the reads, which find much of what is shared in the caches.  us, shared once / every sequence for
@@ -494,7 +498,8 @@ hipError_t launch_paged_decode(const PagedView &c, const PagedAttention &a, floa
   p.scale_log2 = c.sm_scale * kLog2e;
   p.lead = fminf(8.f / p.scale_log2, 3e38f);
   if (s.shared.slots) launch_shared_rows(p, stream);
-  for (p.head0 = 0; p.head0 < c.group; p.head0 += kPagedHeads) {  // one pass over the rows for up to 16 heads of a group
+  // one pass over the rows for up to 16 heads of a group (131072 rows of 8 KV heads, G = 16 92 us, 17 175, 32 180)
+  for (p.head0 = 0; p.head0 < c.group; p.head0 += kPagedHeads) {
     if (s.shared.slots)
       launch_own<true>(p, stream);
     else

@@ -22,8 +22,8 @@
 // Blocks of 64 rows go global -> registers -> LDS, two blocks ahead of the products (three buffers, one barrier per block);
 // LDS rows are padded to 272 (keys) and 288 (values) bytes.
 // Measured: 64 sequences x 4 heads, 32768 rows, 8 KV heads (256 columns, 134 MB, 34 GFLOP, 52 with the weights' second
-// piece): 67 us = 0.77 PFLOP/s of instructions, the rows read once (135 MB).  Bound by the matrix cores, the vector ALU and
-// LDS in turn (41, 35 and 24 % busy) at the clock that they leave; HBM would take 20 us.
+// piece): 67 to 73 us = 0.77 to 0.71 PFLOP/s of instructions, the rows read once (135 MB).  No unit is full: matrix cores 41 %
+// busy, vector ALU 38, LDS 24; a loop of the matrix instruction would take 31 us, HBM 20.
 #include "dp_attend.hpp"
 #include "dp_device.hpp"
 #include "dp_kernels.hpp"
